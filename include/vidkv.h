@@ -1,7 +1,8 @@
 /*
  * vidkv.h - C ABI of the MI355X (gfx950) VidKV hot path:
  *   sub-2-bit KV-cache codec + single-query GQA decode attention over the
- *   packed cache.
+ *   packed cache; beside it rotary positions on several axes and a cache in
+ *   8 bits with its attention (second half of this file).
  *
  * Method (arXiv 2503.16257): keys are quantized per channel with mixed
  * precision - the n_anom channels of largest range get the 2-bit uniform
@@ -293,6 +294,137 @@ vidkv_status vidkv_saliency_scores(const void *X_v_dev, const void *X_t_dev, int
                                    int32_t n_visual, int32_t n_text, int32_t hidden_dim,
                                    float *scores_dev, void *workspace_dev,
                                    size_t workspace_bytes, void *hip_stream);
+
+/* ---- rotary positions and the 8-bit cache ------------------------------------
+ * What stands beside the packed cache: rotary positions on several axes for the
+ * queries and keys that go into either cache, and a cache that holds keys and
+ * values in 8 bits with one magnitude for each block of 32 tokens and head, for
+ * layers and streams that do not stand the packed one: written token by token or
+ * in bulk, read back, and attended over by any number of queries.
+ *
+ * Tensors of these calls are views [B, heads, tokens, channels] with strides of
+ * their own; the channels of a token lie next to each other.  `data` is 16-byte
+ * aligned device memory and every stride a multiple of 16 bytes (else
+ * VIDKV_EINVAL), so both [B, heads, tokens, D] and the transposed view of what a
+ * projection leaves ([B, tokens, heads, D]) are taken as they are.  Outputs must
+ * not overlap inputs unless stated, nor themselves.  */
+typedef enum { VIDKV_F16 = 0, VIDKV_BF16 = 1, VIDKV_F32 = 2 } vidkv_dtype;
+
+typedef struct vidkv_view {
+  void *data;             /* device */
+  int64_t stride_batch;   /* in elements */
+  int64_t stride_head;
+  int64_t stride_token;
+  int32_t dtype;          /* vidkv_dtype */
+} vidkv_view;
+
+/* Rotary positions: pair i of a head's first rot_dim channels is turned by the
+ * angle pos[axis[i]] * freq_i,
+ *     y1 = x1 cos - x2 sin,   y2 = x2 cos + x1 sin;
+ * the channels behind rot_dim are passed on.  Plain host data, made by
+ * vidkv_rotary_init, never retained; `axis` and `turn` may be set by the caller
+ * (an interleaved order of the axes, scaled frequencies). */
+#define VIDKV_ROTARY_PAIRS 128
+typedef struct vidkv_rotary {
+  int32_t head_dim;       /* 16..256, multiple of 16                             */
+  int32_t rot_dim;        /* 16..head_dim, multiple of 16                        */
+  int32_t adjacent;       /* pair i is channels 0: i and i + rot_dim/2,
+                             1: 2i and 2i + 1                                    */
+  int32_t n_axes;         /* 1..4 rows of positions (time, height, width)        */
+  uint8_t axis[VIDKV_ROTARY_PAIRS];  /* the row that pair i takes its position from */
+  uint64_t turn[VIDKV_ROTARY_PAIRS]; /* freq_i as turns a position, times 2^64 (modulo
+                             2^64): products with a position are exact, so angles of
+                             far positions are as accurate as those of near ones */
+} vidkv_rotary;
+
+/* Host function: fills *rot.  sections[n_axes] (host) are the pairs of each axis,
+ * in order, rot_dim / 2 in all.  freq_i = theta^(-2i / rot_dim) radians a position,
+ * or freq[i] (host, rot_dim / 2 numbers) where that is not NULL. */
+vidkv_status vidkv_rotary_init(vidkv_rotary *rot, int32_t head_dim, int32_t rot_dim,
+                               int32_t adjacent, int32_t n_axes, const int32_t *sections,
+                               double theta, const double *freq);
+
+/* Rotates the queries and keys of the same tokens (either may be NULL).
+ *   pos_dev     in : [n_axes, batch, n_tokens] int32, any values
+ *   q, q_out       : [batch, n_q_heads, n_tokens, head_dim], same dtype; q_out
+ *                    may be the same view as q
+ *   k, k_out       : [batch, n_k_heads, ...] likewise, of q's dtype
+ *   inverse        : 0 turns by +angle; 1 by -angle: undoes the rotation, and is
+ *                    its backward pass (gradients of y in, gradients of x out)
+ * Computed in fp32 (angles to 2^-33 turns), rounded once. */
+vidkv_status vidkv_rotary_apply(const vidkv_rotary *rot, int32_t inverse, int32_t batch,
+                                int32_t n_tokens, const int32_t *pos_dev, int32_t n_q_heads,
+                                const vidkv_view *q, const vidkv_view *q_out, int32_t n_k_heads,
+                                const vidkv_view *k, const vidkv_view *k_out, void *hip_stream);
+
+/* Geometry of an 8-bit cache.  A block is 32 tokens of one head; for K and for V
+ * it holds its magnitude A = max |x|, clamped to 2^-40..2^40, and codes
+ *   code 0 (int8): rint(x * 127 / A), value = code * A / 127
+ *   code 1 (e4m3): the nearest e4m3 number to x * 448 / A, value = that * A / 448
+ * (ties to even in both). */
+typedef struct vidkv_cache8 {
+  int32_t n_layers, batch, n_kv_heads;
+  int32_t n_q_heads;      /* multiple of n_kv_heads, any ratio                   */
+  int32_t head_dim;       /* must be 128                                         */
+  int32_t capacity;       /* tokens a sequence, multiple of 32, >= 32            */
+  int32_t code;           /* 0 int8, 1 e4m3                                      */
+  float softmax_scale;    /* multiplies q.k before the softmax, > 0              */
+} vidkv_cache8;
+
+/* Size queries (host): bytes of the cache buffer of all layers, and of the
+ * workspace of an attention call of up to n_query queries a sequence; 0 when
+ * *p or n_query is invalid.  n_kv_heads and batch at most 65535. */
+size_t vidkv_cache8_bytes(const vidkv_cache8 *p);
+size_t vidkv_cache8_workspace_bytes(const vidkv_cache8 *p, int32_t n_query);
+
+/* Codes the first count[b] of n_tokens new tokens of one layer as tokens
+ * start[b], start[b] + 1, ... of sequence b.  Tokens from start[b] on that the
+ * cache held before are given up.  A block that begins before start[b] keeps its
+ * live tokens: where the new ones raise its magnitude from A to A', their codes c
+ * become the code of value(c) (in the code's units) * A / A'; else they are not
+ * touched.  Codes behind the last new token are left as they were.
+ *   K, V      in : [B, Hkv, n_tokens, 128], fp16 or bf16, both the same dtype;
+ *                  rows from count[b] on are not read
+ *   start_dev in : [B] int32; a negative start writes nothing for the sequence,
+ *                  tokens behind the capacity are dropped
+ *   count_dev in : [B] int32 (values beyond 0..n_tokens are taken as the nearer
+ *                  end), or NULL: n_tokens of every sequence
+ *   rot, pos_dev : both NULL, or the rotation of the keys (head_dim 128) with the
+ *                  positions [n_axes, B, n_tokens] of the new tokens: the cache is
+ *                  the same as after vidkv_rotary_apply on K
+ *   cache_dev in/out: >= vidkv_cache8_bytes(p) bytes, 256-byte aligned, need not
+ *                  be cleared before its first use                              */
+vidkv_status vidkv_cache8_write(const vidkv_cache8 *p, int32_t layer, int32_t n_tokens,
+                                const vidkv_view *K, const vidkv_view *V,
+                                const int32_t *start_dev, const int32_t *count_dev,
+                                const vidkv_rotary *rot, const int32_t *pos_dev,
+                                void *cache_dev, size_t cache_bytes, void *hip_stream);
+
+/* Reads tokens start[b] .. start[b] + n_tokens - 1 of one layer back as values
+ * (fp16, bf16 or fp32; either output may be NULL).  Tokens outside
+ * 0..capacity-1 come as zeros; those never written are unspecified. */
+vidkv_status vidkv_cache8_read(const vidkv_cache8 *p, int32_t layer, int32_t n_tokens,
+                               const int32_t *start_dev, const void *cache_dev,
+                               size_t cache_bytes, const vidkv_view *K, const vidkv_view *V,
+                               void *hip_stream);
+
+/* out = Softmax(scale * q K'^T) V' over the first length[b] tokens of one layer.
+ * The queries are the last ones of the sequence: query i of q_count[b] stands at
+ * token length[b] - q_count[b] + i and, with causal = 1, sees the tokens up to
+ * itself; with causal = 0 all.  A query that sees no token, and the rows from
+ * q_count[b] on, get zeros.
+ *   q         in : [B, Hq, n_query, 128], fp16 or bf16
+ *   out      out : likewise, of q's dtype (fp32 accumulation)
+ *   length_dev in: [B] int32, taken as 0..capacity
+ *   q_count_dev in: [B] int32, taken as 0..n_query; NULL: n_query
+ *   workspace_dev : >= vidkv_cache8_workspace_bytes(p, n_query) bytes, 256-byte
+ *                   aligned                                                     */
+vidkv_status vidkv_cache8_attention(const vidkv_cache8 *p, int32_t layer, int32_t n_query,
+                                    int32_t causal, const vidkv_view *q, const void *cache_dev,
+                                    size_t cache_bytes, const int32_t *length_dev,
+                                    const int32_t *q_count_dev, const vidkv_view *out,
+                                    void *workspace_dev, size_t workspace_bytes,
+                                    void *hip_stream);
 
 /* Measurement aids, not part of the method.  Each takes the arguments of the
  * entry point it is named after, checks them the same way, and launches only

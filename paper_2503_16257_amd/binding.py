@@ -36,6 +36,27 @@ class VidkvParams(C.Structure):
     ]
 
 
+class VidkvView(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride_batch", C.c_int64), ("stride_head", C.c_int64),
+                ("stride_token", C.c_int64), ("dtype", C.c_int32)]
+
+
+ROTARY_PAIRS = 128       # VIDKV_ROTARY_PAIRS
+
+
+class VidkvRotary(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("rot_dim", C.c_int32), ("adjacent", C.c_int32), ("n_axes", C.c_int32),
+                ("axis", C.c_uint8 * ROTARY_PAIRS), ("turn", C.c_uint64 * ROTARY_PAIRS)]
+
+
+CODE_INT8, CODE_E4M3 = 0, 1
+
+
+class VidkvCache8(C.Structure):
+    _fields_ = [("n_layers", C.c_int32), ("batch", C.c_int32), ("n_kv_heads", C.c_int32), ("n_q_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("capacity", C.c_int32), ("code", C.c_int32), ("softmax_scale", C.c_float)]
+
+
 class VidkvSideStream(C.Structure):
     _fields_ = [("hip_stream", C.c_void_p), ("fork_event", C.c_void_p), ("join_event", C.c_void_p)]
 
@@ -118,6 +139,21 @@ def lib() -> C.CDLL:
         L.vidkv_decode_attention_stages.restype = C.c_int
         L.vidkv_calib_copy.argtypes = [vp, vp, sz, vp]
         L.vidkv_calib_copy.restype = C.c_int
+        VP, RP, CP, f64 = C.POINTER(VidkvView), C.POINTER(VidkvRotary), C.POINTER(VidkvCache8), C.c_double
+        L.vidkv_rotary_init.argtypes = [RP, i32, i32, i32, i32, C.POINTER(i32), f64, C.POINTER(f64)]
+        L.vidkv_rotary_init.restype = C.c_int
+        L.vidkv_rotary_apply.argtypes = [RP, i32, i32, i32, vp, i32, VP, VP, i32, VP, VP, vp]
+        L.vidkv_rotary_apply.restype = C.c_int
+        L.vidkv_cache8_bytes.argtypes = [CP]
+        L.vidkv_cache8_bytes.restype = sz
+        L.vidkv_cache8_workspace_bytes.argtypes = [CP, i32]
+        L.vidkv_cache8_workspace_bytes.restype = sz
+        L.vidkv_cache8_write.argtypes = [CP, i32, i32, VP, VP, vp, vp, RP, vp, vp, sz, vp]
+        L.vidkv_cache8_write.restype = C.c_int
+        L.vidkv_cache8_read.argtypes = [CP, i32, i32, vp, vp, sz, VP, VP, vp]
+        L.vidkv_cache8_read.restype = C.c_int
+        L.vidkv_cache8_attention.argtypes = [CP, i32, i32, i32, VP, vp, sz, vp, vp, VP, vp, sz, vp]
+        L.vidkv_cache8_attention.restype = C.c_int
         L.vidkv_status_string.argtypes = [C.c_int]
         L.vidkv_status_string.restype = C.c_char_p
         L.vidkv_abi_version.argtypes = []
@@ -186,11 +222,13 @@ def workspace_bytes(p: VidkvParams, which: int) -> int:
 # another 7.8 against 10.0 and 4.2 against 5.8; the launches are 3 us each), and what follows is kept to a few
 # attribute reads per tensor.  torch's names are looked up once, with the library.
 _Tensor = _f16 = _u8 = _f32 = _i32 = _raw_stream = _cur_device = None
+_dtypes = {}             # of views: torch's to vidkv_dtype
 
 
 def _bind_torch(torch) -> None:
     global _Tensor, _f16, _u8, _f32, _i32, _raw_stream, _cur_device
     _f16, _u8, _f32, _i32 = torch.float16, torch.uint8, torch.float32, torch.int32
+    _dtypes.update({torch.float16: 0, torch.bfloat16: 1, torch.float32: 2})
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     _cur_device = torch.cuda.current_device
     _Tensor = torch.Tensor
@@ -341,6 +379,152 @@ def saliency_scores(X_v, X_t, scores, workspace, stream=None) -> None:
         _ptr(X_v, _f16, "X_v"), _ptr(X_t, _f16, "X_t"), B, Tv, X_t.shape[1], d,
         _ptr(scores, _f32, "scores"), _ptr(workspace, _u8, "workspace"),
         _nbytes(workspace), _stream(stream)), "vidkv_saliency_scores")
+
+
+# ---- rotary positions and the 8-bit cache: views [B, heads, tokens, channels] with strides of their own ----
+
+def _here(t, name):
+    if t.device.index != _cur_device():
+        raise ValueError(f"{name}: is on {t.device}, the current device is cuda:{_cur_device()}")
+
+
+def _arg(t, dtype, name, shape=None):
+    """_ptr of a tensor on the current device (None -> NULL), of `shape` if given."""
+    p = _ptr(t, dtype, name)
+    if t is not None:
+        _here(t, name)
+        if shape is not None and tuple(t.shape) != shape:
+            raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
+    return p
+
+
+def _view(t, name, shape, written=False):
+    """A tensor of any strides whose channels lie next to each other, as a VidkvView (None -> NULL)."""
+    if t is None:
+        return None
+    if not isinstance(t, _Tensor) or not t.is_cuda:
+        raise TypeError(f"{name}: expected a CUDA tensor")
+    _here(t, name)
+    code = _dtypes.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name}: expected float16, bfloat16 or float32, got {t.dtype}")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
+    b, h, n, c = t.stride()
+    if c != 1:
+        raise ValueError(f"{name}: the channels of a token must lie next to each other")
+    # the stride of an axis of one is never used, and torch leaves what it likes there
+    b, h, n = (b if shape[0] > 1 else 0), (h if shape[1] > 1 else 0), (n if shape[2] > 1 else 0)
+    if written and 0 not in shape:
+        extent = shape[3]                      # (axes that nest: any further one steps over what the nearer ones span)
+        for st, size in sorted((abs(st), size) for st, size in ((b, shape[0]), (h, shape[1]), (n, shape[2])) if size > 1):
+            if st < extent:
+                raise ValueError(f"{name}: is written to, and its elements overlap")
+            extent += st * (size - 1)
+    return VidkvView(t.data_ptr(), b, h, n, code)
+
+
+def _ref(v):
+    return None if v is None else C.byref(v)
+
+
+def make_rotary(sections, theta: float = 10000.0, head_dim: int = 128, rot_dim=None, adjacent: bool = False,
+                freq=None) -> VidkvRotary:
+    """vidkv_rotary_init: `sections` pairs of each axis (time, height, width: e.g. 16, 24, 24), frequencies
+    theta^(-2i / rot_dim) or `freq` (radians a position, one for each pair)."""
+    rot_dim = head_dim if rot_dim is None else rot_dim
+    sec = (C.c_int32 * max(len(sections), 1))(*sections)
+    fr = None
+    if freq is not None:
+        if len(freq) != rot_dim // 2:
+            raise ValueError(f"freq: expected {rot_dim // 2} numbers, got {len(freq)}")
+        fr = (C.c_double * len(freq))(*(float(f) for f in freq))
+    r = VidkvRotary()
+    _check((_lib or lib()).vidkv_rotary_init(C.byref(r), head_dim, rot_dim, int(adjacent), len(sections), sec, theta, fr),
+           "vidkv_rotary_init")
+    return r
+
+
+def rotary(rot: VidkvRotary, positions, q, q_out, k=None, k_out=None, inverse: bool = False, stream=None) -> None:
+    """vidkv_rotary_apply: q [B,Hq,n,d] (and k [B,Hk,n,d]) turned by their positions [n_axes,B,n] int32 into q_out, k_out
+    (which may be q and k themselves).  `inverse`: turned back; of gradients, the backward pass.  q or k may be None."""
+    L = _lib or lib()
+    x = q if q is not None else k
+    if x is None:
+        raise ValueError("rotary: neither q nor k")
+    B, n = (x.shape[0], x.shape[2]) if x.dim() == 4 else (-1, -1)
+    d = rot.head_dim
+    hq, hk = (0 if t is None or t.dim() != 4 else t.shape[1] for t in (q, k))
+    v = [_view(q, "q", (B, hq, n, d)), _view(q_out if q is not None else None, "q_out", (B, hq, n, d), True),
+         _view(k, "k", (B, hk, n, d)), _view(k_out if k is not None else None, "k_out", (B, hk, n, d), True)]
+    pos = _arg(positions, _i32, "positions", (rot.n_axes, B, n))
+    if B * n == 0 or hq + hk == 0:
+        return
+    _check(L.vidkv_rotary_apply(C.byref(rot), int(inverse), B, n, pos, hq, _ref(v[0]), _ref(v[1]), hk, _ref(v[2]),
+                                _ref(v[3]), _stream(stream)), "vidkv_rotary_apply")
+
+
+def make_cache8(n_layers, batch, n_kv_heads, n_q_heads, capacity, code=CODE_INT8, softmax_scale=None,
+                head_dim=128) -> VidkvCache8:
+    if softmax_scale is None:
+        softmax_scale = 1.0 / math.sqrt(head_dim)
+    return VidkvCache8(n_layers, batch, n_kv_heads, n_q_heads, head_dim, capacity, code, softmax_scale)
+
+
+def cache8_bytes(p: VidkvCache8) -> int:
+    return lib().vidkv_cache8_bytes(C.byref(p))
+
+
+def cache8_workspace_bytes(p: VidkvCache8, n_query: int) -> int:
+    return lib().vidkv_cache8_workspace_bytes(C.byref(p), n_query)
+
+
+def cache8_write(p: VidkvCache8, layer: int, cache, K, V, start, count=None, rotary=None, positions=None,
+                 stream=None) -> None:
+    """vidkv_cache8_write: K, V [B,Hkv,n,128] fp16 / bf16 coded as tokens start[b].. (int32 [B]) of each sequence, the
+    first count[b] of them; with a VidkvRotary and positions [n_axes,B,n] the keys are turned on the way."""
+    L = _lib or lib()
+    n = K.shape[2] if isinstance(K, _Tensor) and K.dim() == 4 else -1
+    shape = (p.batch, p.n_kv_heads, n, 128)
+    vk, vv = _view(K, "K", shape), _view(V, "V", shape)
+    if rotary is not None and positions is None or rotary is None and positions is not None:
+        raise ValueError("cache8_write: rotary and positions come together")
+    pos = None if rotary is None else _arg(positions, _i32, "positions", (rotary.n_axes, p.batch, n))
+    a = [_arg(start, _i32, "start", (p.batch,)), _arg(count, _i32, "count", (p.batch,)), _ref(rotary), pos,
+         _arg(cache, _u8, "cache"), _nbytes(cache), _stream(stream)]
+    if n == 0:
+        return
+    _check(L.vidkv_cache8_write(C.byref(p), layer, n, _ref(vk), _ref(vv), *a), "vidkv_cache8_write")
+
+
+def cache8_read(p: VidkvCache8, layer: int, cache, start, K, V=None, stream=None) -> None:
+    """vidkv_cache8_read: tokens start[b].. (int32 [B]) as values into K, V [B,Hkv,n,128] (fp16, bf16 or fp32; either
+    may be None)."""
+    L = _lib or lib()
+    x = K if K is not None else V
+    n = x.shape[2] if isinstance(x, _Tensor) and x.dim() == 4 else -1
+    shape = (p.batch, p.n_kv_heads, n, 128)
+    vk, vv = _view(K, "K", shape, True), _view(V, "V", shape, True)
+    a = [_arg(start, _i32, "start", (p.batch,)), _arg(cache, _u8, "cache"), _nbytes(cache)]
+    if n == 0:
+        return
+    _check(L.vidkv_cache8_read(C.byref(p), layer, n, *a, _ref(vk), _ref(vv), _stream(stream)), "vidkv_cache8_read")
+
+
+def cache8_attention(p: VidkvCache8, layer: int, cache, q, out, length, workspace, q_count=None, causal: bool = True,
+                     stream=None) -> None:
+    """vidkv_cache8_attention: queries q [B,Hq,n,128], the last tokens of each sequence, over its first length[b] (int32
+    [B]) tokens of the cache -> out; q_count[b]: how many of them there are (None: all n)."""
+    L = _lib or lib()
+    n = q.shape[2] if isinstance(q, _Tensor) and q.dim() == 4 else -1
+    shape = (p.batch, p.n_q_heads, n, 128)
+    vq, vo = _view(q, "q", shape), _view(out, "out", shape, True)
+    a = [_arg(cache, _u8, "cache"), _nbytes(cache), _arg(length, _i32, "length", (p.batch,)),
+         _arg(q_count, _i32, "q_count", (p.batch,)), _ref(vo), _arg(workspace, _u8, "workspace"), _nbytes(workspace)]
+    if n == 0:
+        return
+    _check(L.vidkv_cache8_attention(C.byref(p), layer, n, int(causal), _ref(vq), *a, _stream(stream)),
+           "vidkv_cache8_attention")
 
 
 def calib_copy(dst, src, stream=None) -> None:

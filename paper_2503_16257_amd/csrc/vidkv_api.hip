@@ -90,9 +90,11 @@ bool side_malformed(const vidkv_side_stream* s) {
   return s && !(s->hip_stream && s->fork_event && s->join_event);
 }
 
+}  // namespace
+
 // A stream of another device than the current one cannot take this call's launches.
 // (The NULL stream belongs to the current device.  If the runtime cannot tell, go on.)
-bool stream_on_current_device(hipStream_t st) {
+bool vidkv::stream_on_current_device(hipStream_t st) {
   if (!st) return true;
   int cur = 0, dev = 0;
   if (hipGetDevice(&cur) != hipSuccess || hipStreamGetDevice(st, &dev) != hipSuccess) {
@@ -101,7 +103,6 @@ bool stream_on_current_device(hipStream_t st) {
   }
   return cur == dev;
 }
-}  // namespace
 
 extern "C" {
 

@@ -72,6 +72,9 @@ struct EncodeSpan {
 // Compute units of the current device (decode_attn.hip).
 int device_cu_count();
 
+// Whether a stream can take this call's launches: it belongs to the current device (vidkv_api.hip).
+bool stream_on_current_device(hipStream_t st);
+
 __host__ __device__ inline size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 inline bool make_geom(const vidkv_params* p, Geom* g) {
