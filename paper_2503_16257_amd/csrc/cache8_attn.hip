@@ -10,6 +10,7 @@
 // that a P of 2^-29 of the largest still has fp16's 11 bits.
 // bf16 queries become fp16 operands under a power of two of their own row.
 #include "cache8.h"
+#include <algorithm>
 
 namespace vidkv {
 
@@ -26,7 +27,7 @@ struct C8Attn {
   const int32_t* q_count;      // or nullptr
   float* po;                   // partials [B * H * rows][splits][128], [..][splits][2]; nullptr: one split, straight to out
   float* pml;
-  int H, rep, n, cap, nbc, splits, causal, bf16;
+  int B, H, rep, n, cap, nbc, splits, causal, bf16;
   float scale2;                // softmax scale * log2 e / level
   float inv_level;
 };
@@ -132,37 +133,43 @@ __device__ __forceinline__ void load_rows(Rows<NT>& r, const C8Attn& a, int b, i
   }
 }
 
-// One block's tokens t0 .. t0 + 31 into the running sums.  EDGE: some row does not see all of them.
-template <int NT, int CODE, bool EDGE>
-__device__ __forceinline__ void take_block(Rows<NT>& r, const Block& f, int t0, int len, int lane) {
+#define SB __builtin_amdgcn_sched_barrier(0)
+// One block's tokens t0 .. t0 + 31 into the running sums; k(tt, j), v(m): its operands, tile of 16 tokens and 32 channels
+// of them, tile of 16 channels.  edge: some row does not see all of its tokens.
+template <int NT, class K, class V>
+__device__ __forceinline__ void take_block(Rows<NT>& r, const K& k, const V& v, float km, float vm, bool edge, int t0,
+                                           int lane) {
   const int kb = lane >> 4;
+  // operands are asked for two ahead of their products, and the order is held: left to itself the compiler asks for all of
+  // them at once and has no registers left
   f4 s[NT][2];
+  Op n0 = k(0, 0), n1 = k(0, 1);
 #pragma unroll
-  for (int tt = 0; tt < 2; ++tt) {
+  for (int g = 0; g < 4; ++g) {
+    const Op o0 = n0, o1 = n1;
+    if (g < 3) { n0 = k((g + 1) >> 1, 2 * ((g + 1) & 1)); n1 = k((g + 1) >> 1, 2 * ((g + 1) & 1) + 1); }
+    else { n0 = v(0); n1 = v(1); }
+    SB;
 #pragma unroll
-    for (int t = 0; t < NT; ++t) s[t][tt] = f4{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < NT; ++t) s[t][g >> 1] = mma(o0, r.q[t][2 * (g & 1)], g & 1 ? s[t][g >> 1] : f4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const u32x4 w = f.k[2 * tt + (j >> 1)];
-      const Op k = decode8<CODE>(w[2 * (j & 1)], w[2 * (j & 1) + 1]);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) s[t][tt] = mma(k, r.q[t][j], s[t][tt]);
-    }
+    for (int t = 0; t < NT; ++t) s[t][g >> 1] = mma(o1, r.q[t][2 * (g & 1) + 1], s[t][g >> 1]);
+    SB;
   }
-  const float lv = __log2f(f.vm) + UP, rv = __builtin_amdgcn_rcpf(f.vm);
+  const float lv = __log2f(vm), rv = __builtin_amdgcn_rcpf(vm);
   Op p[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    const float ck = r.cq[t] * f.km;
-    float y[8], big = -INFINITY;
+    const float ck = r.cq[t] * km;
+    if (edge) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float v = s[t][i >> 2][i & 3] * ck;
-      if (EDGE) v = t0 + slot_token(kb, i) < r.limit[t] ? v : -INFINITY;
-      y[i] = v;
-      big = fmaxf(big, v);
+      for (int i = 0; i < 8; ++i)
+        if (t0 + slot_token(kb, i) >= r.limit[t]) s[t][i >> 2][i & 3] = -INFINITY;
     }
-    const float top = big + lv - UP;
+    float big = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) big = fmaxf(big, s[t][i >> 2][i & 3]);
+    const float top = fmaf(big, ck, lv);
     if (__any(top > r.m[t] + RISE)) {
       const float mn = fmaxf(r.m[t], max16(max32(top)));
       const float al = __builtin_amdgcn_exp2f(r.m[t] - mn);
@@ -171,29 +178,49 @@ __device__ __forceinline__ void take_block(Rows<NT>& r, const Block& f, int t0, 
 #pragma unroll
       for (int m = 0; m < 8; ++m) r.o[t][m] *= al;
     }
-    const float off = lv - r.m[t];
+    const float off = lv + UP - r.m[t];
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      y[i] = __builtin_amdgcn_exp2f(y[i] + off);
-      sum += y[i];
+      const float e = __builtin_amdgcn_exp2f(fmaf(s[t][i >> 2][i & 3], ck, off));
+      sum += e;
+      p[t].v[i] = (_Float16)e;
     }
     r.l[t] = fmaf(sum, rv, r.l[t]);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) p[t].v[i] = (_Float16)y[i];
+    SB;
   }
 #pragma unroll
-  for (int m = 0; m < 8; ++m) {
-    uint32_t u0 = f.v[m >> 1][2 * (m & 1)], u1 = f.v[m >> 1][2 * (m & 1) + 1];
-    if (EDGE && CODE == 1) {               // bytes behind the length can be a NaN's
-      const int n0 = len - t0 - 4 * kb, n1 = n0 - 16;
-      u0 = n0 >= 4 ? u0 : n0 <= 0 ? 0u : u0 & ((1u << (8 * n0)) - 1);
-      u1 = n1 >= 4 ? u1 : n1 <= 0 ? 0u : u1 & ((1u << (8 * n1)) - 1);
-    }
-    const Op v = decode8<CODE>(u0, u1);
+  for (int m = 0; m < 8; m += 2) {
+    const Op o0 = n0, o1 = n1;
+    if (m < 6) { n0 = v(m + 2); n1 = v(m + 3); }
+    SB;
 #pragma unroll
-    for (int t = 0; t < NT; ++t) r.o[t][m] = mma(v, p[t], r.o[t][m]);
+    for (int t = 0; t < NT; ++t) r.o[t][m] = mma(o0, p[t], r.o[t][m]);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) r.o[t][m + 1] = mma(o1, p[t], r.o[t][m + 1]);
+    SB;
   }
+}
+
+// The bytes of V codes (a lane group's eight tokens of a block, u0 and u1) of tokens that are there: n0 of the first four,
+// n1 of the others.  What lies behind the length can be a NaN's code.
+__device__ __forceinline__ uint32_t live(uint32_t u, int n) { return n >= 4 ? u : n <= 0 ? 0u : u & ((1u << (8 * n)) - 1); }
+
+// A block out of a lane's registers.
+template <int NT, int CODE>
+__device__ __forceinline__ void take_codes(Rows<NT>& r, const Block& f, bool edge, int t0, int len, int lane) {
+  const int n0 = len - t0 - 4 * (lane >> 4), n1 = n0 - 16;
+  take_block<NT>(
+      r, [&](int tt, int j) {
+        const u32x4 w = f.k[2 * tt + (j >> 1)];
+        return decode8<CODE>(w[2 * (j & 1)], w[2 * (j & 1) + 1]);
+      },
+      [&](int m) {
+        uint32_t u0 = f.v[m >> 1][2 * (m & 1)], u1 = f.v[m >> 1][2 * (m & 1) + 1];
+        if (CODE == 1 && edge) { u0 = live(u0, n0); u1 = live(u1, n1); }
+        return decode8<CODE>(u0, u1);
+      },
+      f.km, f.vm, edge, t0, lane);
 }
 
 __device__ __forceinline__ void put_out(const C8Attn& a, int b, int h, int row, int c, const f4& v) {
@@ -228,8 +255,7 @@ __global__ __launch_bounds__(256) void c8_few_kernel(C8Attn a) {
     load_block(f, a.kc, a.vc, a.km, a.vm, head + b0, lane);
     for (int i = b0; i < b1; ++i) {
       if (i + 1 < b1) load_block(g, a.kc, a.vc, a.km, a.vm, head + i + 1, lane);
-      if ((i + 1) * G <= all) take_block<NT, CODE, false>(r, f, i * G, len, lane);
-      else take_block<NT, CODE, true>(r, f, i * G, len, lane);
+      take_codes<NT, CODE>(r, f, (i + 1) * G > all, i * G, len, lane);
       f = g;
     }
   }
@@ -267,41 +293,224 @@ __global__ __launch_bounds__(256) void c8_few_kernel(C8Attn a) {
   }
 }
 
-// Waves share out the rows: 16 NT a wave, 64 NT a workgroup, each walking the split's blocks.
-// grid (row tiles x splits, H, B); the tiles that see most come first.
+// Waves share out the rows: 16 NT a wave, 64 NT a workgroup, which walks the split's blocks together.  Each wave
+// decodes a quarter of a block into LDS, where all four read it as operands, in their order, 16 bytes a lane.  The vector
+// units are the bound, not the matrix cores: a 16 x 16 x 32 product keeps them from issuing for 8 of its 16 cycles, and a
+// block costs a wave some 170 instructions of 4.6 cycles beside 51 products (a score: 1 multiply-add, an exponential of 8.6
+// cycles, half a conversion, half a maximum; the decoding 40).  So: the more rows a wave, the fewer decodings and LDS reads a
+// row - 48 rows are what 256 registers hold, two waves a SIMD (32 rows, three waves: 410 us where this took 352) - the
+// weights of a block are made between the products of the block before, the decoding between those of the scores, and the
+// denominators are products with ones.  196 queries x 28 heads over 98196 tokens, int8: 327 us, 0.84 PFLOP/s (0.94 with the
+// rows that pad the last tile); 6272 over themselves, causal: 321 us, 0.88.
+// grid (tiles of rows x splits x B x H), heads fastest: the tiles that see most come first, and what shares a head's
+// codes runs at the same time, where the heads divide the eight dies' turns on the same die.
 template <int NT, int CODE>
-__global__ __launch_bounds__(256) void c8_many_kernel(C8Attn a, int tiles) {
-  const int b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
-  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+__global__ __launch_bounds__(256, 2) void c8_many_kernel(C8Attn a, int tiles) {
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int x = lane & 15, kb = lane >> 4;
-  const int tile = tiles - 1 - blockIdx.x / a.splits, sp = blockIdx.x % a.splits;
+  int at = blockIdx.x;
+  const int h = at % a.H; at /= a.H;
+  const int b = at % a.B; at /= a.B;
+  const int sp = at % a.splits, tile = tiles - 1 - at / a.splits;
   const int len = min(max(a.length[b], 0), a.cap);
   const int nq = a.q_count ? min(max(a.q_count[b], 0), a.n) : a.n;
-  const int rows = a.n * a.rep, row0 = tile * 64 * NT + w * 16 * NT;
-  if (row0 >= rows) return;
+  const int rows = a.n * a.rep, tile0 = tile * 64 * NT, row0 = tile0 + w * 16 * NT;
   Rows<NT> r;
   load_rows<NT>(r, a, b, h, row0, rows, len, nq, lane);
-  // tokens that the first of the wave's rows sees, and those that its last does
-  const int i0 = row0 / a.rep, i1 = min((row0 + 16 * NT - 1) / a.rep, nq - 1);
-  const int all = i1 < i0 ? 0 : a.causal ? max(len - nq + i0 + 1, 0) : len;
-  const int most = i1 < i0 ? 0 : a.causal ? max(len - nq + i1 + 1, 0) : len;
-  const int nb = (most + G - 1) / G;
+  // tokens that the first row from `row` on sees, and those that the last of `n` rows does
+  auto least = [&](int row) { return row / a.rep >= nq ? 0 : a.causal ? max(len - nq + row / a.rep + 1, 0) : len; };
+  auto most = [&](int row, int n) {
+    const int i1 = min((row + n - 1) / a.rep, nq - 1);
+    return i1 < row / a.rep ? 0 : a.causal ? max(len - nq + i1 + 1, 0) : len;
+  };
+  const int all = least(row0), nb = (most(tile0, 64 * NT) + G - 1) / G;
   const int b0 = (int)((long long)sp * nb / a.splits), b1 = (int)((long long)(sp + 1) * nb / a.splits);
   const size_t head = ((size_t)b * a.H + h) * a.nbc;
+  __shared__ Op ops[2][16][64];            // 0..7: K, tile of tokens tt, channels j at 4 tt + j; 8..15: V, tile of channels
+  // this wave's quarter: K piece w (tt = w >> 1, j = 2 (w & 1) and the next), V piece w (m = 2 w and the next)
+  const uint8_t* kc = a.kc + head * C8REC + ((w >> 1) * 16 + x) * D + (w & 1) * 64 + kb * 16;
+  const uint8_t* vc = a.vc + head * C8REC + w * 1024 + lane * 16;
+  u32x4 gk, gv;                            // codes on their way to LDS
+  float gkm, gvm;                          // magnitudes of the block in gk
+  auto ask_k = [&](int i) {
+    i = min(i, b1 - 1);
+    gk = *reinterpret_cast<const u32x4*>(kc + (size_t)i * C8REC);
+    gkm = a.km[head + i];
+    gvm = a.vm[head + i];
+  };
+  auto ask_v = [&](int i) { gv = *reinterpret_cast<const u32x4*>(vc + (size_t)min(i, b1 - 1) * C8REC); };
+  auto clear_dead = [&](int i) {           // tokens behind the length
+    if (CODE == 1 && (i + 1) * G > len) {
+      const int n0 = len - i * G - 4 * kb, n1 = n0 - 16;
+      gv[0] = live(gv[0], n0); gv[1] = live(gv[1], n1);
+      gv[2] = live(gv[2], n0); gv[3] = live(gv[3], n1);
+    }
+  };
+  auto put_k = [&](int i, int e) { ops[i & 1][2 * w + e][lane] = decode8<CODE>(gk[2 * e], gk[2 * e + 1]); };
+  auto put_v = [&](int i, int e) { ops[i & 1][8 + 2 * w + e][lane] = decode8<CODE>(gv[2 * e], gv[2 * e + 1]); };
+  // LDS alone is handed over: what is still on its way from memory goes on
+  auto hand_over = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+  f4 s[NT][2];
+  Op p[NT], n0, n1;
+  float al[NT];
+  Op ones;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) ones.u[i] = 0x3c003c00u;
+  // x of block i; between its products, what goes to LDS meanwhile: fill(0..3)
+  auto scores = [&](int i, auto&& fill) {
+    const Op(*o)[64] = ops[i & 1];
+    n0 = o[0][lane];
+    n1 = o[1][lane];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const Op o0 = n0, o1 = n1;
+      if (g < 3) { n0 = o[2 * g + 2][lane]; n1 = o[2 * g + 3][lane]; }
+      SB;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) s[t][g >> 1] = mma(o0, r.q[t][2 * (g & 1)], g & 1 ? s[t][g >> 1] : f4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+      for (int t = 0; t < NT; ++t) s[t][g >> 1] = mma(o1, r.q[t][2 * (g & 1) + 1], s[t][g >> 1]);
+      fill(g);
+#pragma unroll
+      for (int t = 0; t < 2 * NT; ++t) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x2, 2, 0);
+      }
+      SB;
+    }
+  };
+  // the weights' sum over a block's tokens, as a product with ones: every element of the tile is it
+  auto sums = [&](float rv) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) r.l[t] = fmaf(mma(ones, p[t], f4{0.f, 0.f, 0.f, 0.f})[0], rv, r.l[t]);
+  };
+  // masks, and the maxima where they have to rise; true: o is to be multiplied by al
+  auto maxima = [&](int i, float km, float lv) {
+    const int t0 = i * G;
+    if (t0 + G > all) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (t0 + slot_token(kb, k) >= r.limit[t]) s[t][k >> 2][k & 3] = -INFINITY;
+    }
+    float top[NT];
+    bool rise = false;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      float big = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) big = fmaxf(big, s[t][k >> 2][k & 3]);
+      top[t] = fmaf(big, r.cq[t] * km, lv);
+      rise = rise || top[t] > r.m[t] + RISE;
+    }
+    rise = __any(rise);
+    if (rise) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const float mn = fmaxf(r.m[t], max16(max32(top[t])));
+        al[t] = __builtin_amdgcn_exp2f(r.m[t] - mn);
+        r.m[t] = mn;
+        r.l[t] *= al[t];
+      }
+    }
+    return rise;
+  };
+  // one score of the block as a weight
+  float e0, ck[NT], off[NT];
+  Op pn[NT];
+  auto weight = [&](int t, int k) {
+    const float e = __builtin_amdgcn_exp2f(fmaf(s[t][k >> 2][k & 3], ck[t], off[t]));
+    if (k & 1) pn[t].p[k >> 1] = h2{(_Float16)e0, (_Float16)e};
+    else e0 = e;
+  };
+  auto factors = [&](float km, float lv) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) { ck[t] = r.cq[t] * km; off[t] = lv + UP - r.m[t]; }
+  };
   if (b0 < b1) {
-    Block f, g;
-    load_block(f, a.kc, a.vc, a.km, a.vm, head + b0, lane);
-    for (int i = b0; i < b1; ++i) {
-      if (i + 1 < b1) load_block(g, a.kc, a.vc, a.km, a.vm, head + i + 1, lane);
-      if ((i + 1) * G <= all) take_block<NT, CODE, false>(r, f, i * G, len, lane);
-      else take_block<NT, CODE, true>(r, f, i * G, len, lane);
-      f = g;
+    ask_k(b0);
+    ask_v(b0);
+    clear_dead(b0);
+    put_k(b0, 0); put_k(b0, 1);
+    put_v(b0, 0); put_v(b0, 1);
+    float km = gkm, vm = gvm;
+    ask_k(b0 + 1);
+    put_k(b0 + 1, 0); put_k(b0 + 1, 1);
+    float kn = gkm, vn = gvm;              // of the next block
+    ask_k(b0 + 2);
+    ask_v(b0 + 1);
+    hand_over();
+    scores(b0, [](int) {});
+    float lv = __log2f(vm);
+    maxima(b0, km, lv);
+    factors(km, lv);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) weight(t, k);
+      p[t] = pn[t];
+    }
+    float rv = __builtin_amdgcn_rcpf(vm);
+    hand_over();
+    // the weights of block i are there; block i + 1 is scored, and turned into weights between the products of block i
+    for (int i = b0; i + 1 < b1; ++i) {
+      km = kn; vm = vn;
+      kn = gkm; vn = gvm;
+      clear_dead(i + 1);
+      scores(i + 1, [&](int g) {
+        if (g < 2) put_k(i + 2, g);
+        else put_v(i + 1, g - 2);
+      });
+      ask_k(i + 3);
+      ask_v(i + 2);
+      sums(rv);
+      rv = __builtin_amdgcn_rcpf(vm);
+      lv = __log2f(vm);
+      const bool rise = maxima(i + 1, km, lv);
+      factors(km, lv);
+      const Op(*o)[64] = ops[i & 1] + 8;
+      n0 = o[0][lane];
+      n1 = o[1][lane];
+      SB;
+#pragma unroll
+      for (int m = 0; m < 8; m += 2) {
+        const Op o0 = n0, o1 = n1;
+        if (m < 6) { n0 = o[m + 2][lane]; n1 = o[m + 3][lane]; }
+#pragma unroll
+        for (int t = 0; t < 2 * NT; ++t) {
+          const int at = m * NT + t;
+          r.o[t % NT][m + t / NT] = mma(t < NT ? o0 : o1, p[t % NT], r.o[t % NT][m + t / NT]);
+          weight(at >> 3, at & 7);
+          SB;
+        }
+      }
+      // (else the compiler moves all of this behind the branch)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) asm volatile("" : "+v"(pn[t].q));
+#pragma unroll
+      for (int t = 0; t < NT; ++t) p[t] = pn[t];
+      if (rise) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int m = 0; m < 8; ++m) r.o[t][m] *= al[t];
+      }
+      hand_over();
+    }
+    sums(rv);
+    const Op(*o)[64] = ops[(b1 - 1) & 1] + 8;
+#pragma unroll
+    for (int m = 0; m < 8; ++m) {
+      const Op v = o[m][lane];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) r.o[t][m] = mma(v, p[t], r.o[t][m]);
     }
   }
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const int row = row0 + 16 * t + x;
-    const float l = row_sum(r, t);
+    const float l = r.limit[t] > 0 ? r.l[t] : 0.0f;
     if (row >= rows) continue;
     if (a.po) {
       const size_t at = (((size_t)b * a.H + h) * rows + row) * a.splits + sp;
@@ -316,22 +525,61 @@ __global__ __launch_bounds__(256) void c8_many_kernel(C8Attn a, int tiles) {
   }
 }
 
-// out of the splits' partials: 32 lanes a row, eight rows a workgroup.  grid (ceil(rows / 8), H, B).
+// out of the splits' partials.  A row is taken by 32 SL threads, 32 channel quads x SL slices of its splits, eight
+// splits asked for at a time; 256 / (32 SL) rows a workgroup.  grid (ceil(rows / rows a workgroup), H, B).
+template <int SL>
 __global__ __launch_bounds__(256) void c8_merge_kernel(C8Attn a) {
-  const int b = blockIdx.z, h = blockIdx.y, c4 = threadIdx.x & 31;
-  const int rows = a.n * a.rep, row = blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (row >= rows) return;
-  const size_t at = (((size_t)b * a.H + h) * rows + row) * a.splits;
-  float M = NONE;
-  for (int s = 0; s < a.splits; ++s) M = fmaxf(M, a.pml[2 * (at + s)]);
+  const int b = blockIdx.z, h = blockIdx.y, c4 = threadIdx.x & 31, sl = (threadIdx.x >> 5) % SL, rr = (threadIdx.x >> 5) / SL;
+  const int rows = a.n * a.rep, row = blockIdx.x * (8 / SL) + rr;
+  const bool on = row < rows;
+  const size_t at = (((size_t)b * a.H + h) * rows + (on ? row : 0)) * a.splits;
+  const f4* po = reinterpret_cast<const f4*>(a.po) + at * (D / 4) + c4;
+  const f2* pm = reinterpret_cast<const f2*>(a.pml) + at;
+  float M = NONE, l = 0.0f;
   f4 o = f4{0.f, 0.f, 0.f, 0.f};
-  float l = 0.0f;
-  for (int s = 0; s < a.splits; ++s) {
-    const float wt = __builtin_amdgcn_exp2f(a.pml[2 * (at + s)] - M);
-    o += reinterpret_cast<const f4*>(a.po)[(at + s) * (D / 4) + c4] * wt;
-    l = fmaf(a.pml[2 * (at + s) + 1], wt, l);
+  for (int s0 = sl; s0 < a.splits; s0 += 8 * SL) {
+    f4 v[8];
+    f2 ml[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int s = min(s0 + u * SL, a.splits - 1);           // (behind the last: a split again, not counted)
+      ml[u] = pm[s];
+      v[u] = po[(size_t)s * (D / 4)];
+    }
+    float top = M;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) top = fmaxf(top, ml[u][0]);
+    const float al = __builtin_amdgcn_exp2f(M - top);
+    M = top;
+    o *= al;
+    l *= al;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const float wt = s0 + u * SL < a.splits ? __builtin_amdgcn_exp2f(ml[u][0] - M) : 0.0f;
+      o += v[u] * wt;
+      l = fmaf(ml[u][1], wt, l);
+    }
   }
-  put_out(a, b, h, row, 4 * c4, l != 0.0f ? o * (a.inv_level / l) : f4{0.f, 0.f, 0.f, 0.f});
+  if constexpr (SL > 1) {
+    __shared__ f4 so[8][32];
+    __shared__ float sm[8], sl_[8];
+    const int k = threadIdx.x >> 5;
+    so[k][c4] = o;
+    if (c4 == 0) { sm[k] = M; sl_[k] = l; }
+    __syncthreads();
+    if (sl != 0) return;
+    const int k0 = rr * SL;
+    M = NONE;
+    for (int i = 0; i < SL; ++i) M = fmaxf(M, sm[k0 + i]);
+    o = f4{0.f, 0.f, 0.f, 0.f};
+    l = 0.0f;
+    for (int i = 0; i < SL; ++i) {
+      const float wt = __builtin_amdgcn_exp2f(sm[k0 + i] - M);
+      o += so[k0 + i][c4] * wt;
+      l = fmaf(sl_[k0 + i], wt, l);
+    }
+  }
+  if (on) put_out(a, b, h, row, 4 * c4, l != 0.0f ? o * (a.inv_level / l) : f4{0.f, 0.f, 0.f, 0.f});
 }
 
 // How a call is shared out.
@@ -345,9 +593,11 @@ static C8Plan c8_plan(const C8Geom& g, int n) {
   C8Plan p{};
   const long long rows = (long long)n * g.rep;
   p.few = rows <= 32;
-  p.nt = p.few && rows <= 16 ? 1 : 2;
+  p.nt = !p.few ? 3 : rows <= 16 ? 1 : 2;
   p.tiles = p.few ? 1 : (int)((rows + 64 * p.nt - 1) / (64 * p.nt));
-  const long long wgs = (long long)p.tiles * g.H * g.B, want = 4LL * device_cu_count();
+  // two workgroups a compute unit; four where waves share blocks and the sequences' lengths can differ (one layer of 64
+  // sequences of 12544 to 25088 tokens: 170 us with two, 160 with four; one of 196000: 39.0 and 39.8, the merge 4.1 and 5.9)
+  const long long wgs = (long long)p.tiles * g.H * g.B, want = (p.few && g.B > 1 ? 4LL : 2LL) * device_cu_count();
   long long s = (want + wgs - 1) / wgs;
   const long long most = p.few ? (g.nbc + 3) / 4 : (g.nbc + 7) / 8;
   p.splits = (int)std::max(1LL, std::min({s, most, 256LL}));
@@ -376,7 +626,7 @@ hipError_t launch_c8_attn(const C8Geom& g, int layer, int n, int causal, float s
     a.po = static_cast<float*>(ws);
     a.pml = a.po + (size_t)g.B * g.Hq * n * p.splits * D;
   }
-  a.H = g.H; a.rep = g.rep; a.n = n; a.cap = g.cap; a.nbc = g.nbc; a.splits = p.splits; a.causal = causal;
+  a.B = g.B; a.H = g.H; a.rep = g.rep; a.n = n; a.cap = g.cap; a.nbc = g.nbc; a.splits = p.splits; a.causal = causal;
   a.bf16 = q->dtype == VIDKV_BF16;
   const float level = g.code == 0 ? 127.0f : 448.0f;
   a.scale2 = scale * 1.4426950408889634f / level;
@@ -387,13 +637,14 @@ hipError_t launch_c8_attn(const C8Geom& g, int layer, int n, int causal, float s
     const dim3 few(p.splits, g.H, g.B);
     if (p.few && p.nt == 1) hipLaunchKernelGGL((c8_few_kernel<1, CODE>), few, blk, 0, st, a);
     else if (p.few) hipLaunchKernelGGL((c8_few_kernel<2, CODE>), few, blk, 0, st, a);
-    else hipLaunchKernelGGL((c8_many_kernel<2, CODE>), dim3(p.tiles * p.splits, g.H, g.B), blk, 0, st, a, p.tiles);
+    else hipLaunchKernelGGL((c8_many_kernel<3, CODE>), dim3(p.tiles * p.splits * g.H * g.B), blk, 0, st, a, p.tiles);
   };
   if (g.code == 0) by_code(std::integral_constant<int, 0>{});
   else by_code(std::integral_constant<int, 1>{});
   if (a.po) {
     const int rows = n * g.rep;
-    hipLaunchKernelGGL(c8_merge_kernel, dim3((rows + 7) / 8, g.H, g.B), blk, 0, st, a);
+    if (p.splits > 8) hipLaunchKernelGGL(c8_merge_kernel<8>, dim3(rows, g.H, g.B), blk, 0, st, a);
+    else hipLaunchKernelGGL(c8_merge_kernel<1>, dim3((rows + 7) / 8, g.H, g.B), blk, 0, st, a);
   }
   return hipGetLastError();
 }
