@@ -185,6 +185,9 @@ def _load_native(L):
     m.bind(*(C.cast(f, C.c_void_p).value for f in (
         L.vidkv_decode_attention, L.vidkv_decode_attention_noalloc, L.vidkv_flush_residual)),
         VidkvParams, VidkvSideStream)
+    m.bind8(*(C.cast(f, C.c_void_p).value for f in (
+        L.vidkv_rotary_apply, L.vidkv_cache8_write, L.vidkv_cache8_read, L.vidkv_cache8_attention)),
+        VidkvRotary, VidkvCache8)
     return m
 
 
@@ -449,6 +452,10 @@ def rotary(rot: VidkvRotary, positions, q, q_out, k=None, k_out=None, inverse: b
     """vidkv_rotary_apply: q [B,Hq,n,d] (and k [B,Hk,n,d]) turned by their positions [n_axes,B,n] int32 into q_out, k_out
     (which may be q and k themselves).  `inverse`: turned back; of gradients, the backward pass.  q or k may be None."""
     L = _lib or lib()
+    if _native is not None:
+        st = _native.rotary(rot, positions, q, q_out, k, k_out, inverse, _stream, stream)
+        if st is not None:
+            return _check(st, "vidkv_rotary_apply")
     x = q if q is not None else k
     if x is None:
         raise ValueError("rotary: neither q nor k")
@@ -484,6 +491,10 @@ def cache8_write(p: VidkvCache8, layer: int, cache, K, V, start, count=None, rot
     """vidkv_cache8_write: K, V [B,Hkv,n,128] fp16 / bf16 coded as tokens start[b].. (int32 [B]) of each sequence, the
     first count[b] of them; with a VidkvRotary and positions [n_axes,B,n] the keys are turned on the way."""
     L = _lib or lib()
+    if _native is not None:
+        st = _native.cache8_write(p, layer, cache, K, V, start, count, rotary, positions, _stream, stream)
+        if st is not None:
+            return _check(st, "vidkv_cache8_write")
     n = K.shape[2] if isinstance(K, _Tensor) and K.dim() == 4 else -1
     shape = (p.batch, p.n_kv_heads, n, 128)
     vk, vv = _view(K, "K", shape), _view(V, "V", shape)
@@ -501,6 +512,10 @@ def cache8_read(p: VidkvCache8, layer: int, cache, start, K, V=None, stream=None
     """vidkv_cache8_read: tokens start[b].. (int32 [B]) as values into K, V [B,Hkv,n,128] (fp16, bf16 or fp32; either
     may be None)."""
     L = _lib or lib()
+    if _native is not None:
+        st = _native.cache8_read(p, layer, cache, start, K, V, _stream, stream)
+        if st is not None:
+            return _check(st, "vidkv_cache8_read")
     x = K if K is not None else V
     n = x.shape[2] if isinstance(x, _Tensor) and x.dim() == 4 else -1
     shape = (p.batch, p.n_kv_heads, n, 128)
@@ -516,6 +531,10 @@ def cache8_attention(p: VidkvCache8, layer: int, cache, q, out, length, workspac
     """vidkv_cache8_attention: queries q [B,Hq,n,128], the last tokens of each sequence, over its first length[b] (int32
     [B]) tokens of the cache -> out; q_count[b]: how many of them there are (None: all n)."""
     L = _lib or lib()
+    if _native is not None:
+        st = _native.cache8_attention(p, layer, cache, q, out, length, workspace, q_count, causal, _stream, stream)
+        if st is not None:
+            return _check(st, "vidkv_cache8_attention")
     n = q.shape[2] if isinstance(q, _Tensor) and q.dim() == 4 else -1
     shape = (p.batch, p.n_q_heads, n, 128)
     vq, vo = _view(q, "q", shape), _view(out, "out", shape, True)

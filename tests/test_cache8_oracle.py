@@ -194,3 +194,26 @@ def test_binding_refuses_host_tensors():
         vk.cache8_read(p, 0, torch.zeros(8, dtype=torch.uint8), i, x, x)
     with pytest.raises(TypeError):
         vk.cache8_attention(p, 0, torch.zeros(8, dtype=torch.uint8), x, x, i, torch.zeros(256, dtype=torch.uint8))
+
+
+def test_odd_arguments_are_left_to_the_python_path():
+    """The native call layer takes plain arguments that pass, and no others."""
+    vk.lib()
+    n = vk._native
+    assert n.rotary(*[None] * 9) is None and n.rotary(1) is None
+    assert n.cache8_write(*[None] * 11) is None and n.cache8_read(*[None] * 8) is None
+    assert n.cache8_attention(*[None] * 11) is None
+    with pytest.raises(TypeError):
+        n.bind8(1, 2)
+    x = torch.zeros((1, 2, 3, 128), dtype=torch.float16)
+    i = torch.zeros(1, dtype=torch.int32)
+    u = torch.zeros(4096, dtype=torch.uint8)
+    rot, p = vk.make_rotary((64,)), vk.make_cache8(1, 1, 2, 2, 32)
+    pos = torch.zeros((1, 1, 3), dtype=torch.int32)
+    for r in (rot, bytes(C.sizeof(vk.VidkvRotary)), p):                      # host tensors; foreign structures
+        assert n.rotary(r, pos, x, x, None, None, False, vk._stream, None) is None
+    for c in (p, bytes(C.sizeof(vk.VidkvCache8)), rot):
+        assert n.cache8_write(c, 0, u, x, x, i, None, rot, pos, vk._stream, None) is None
+        assert n.cache8_write(c, 0, u, x, x, i, None, None, None, vk._stream, None) is None
+        assert n.cache8_read(c, 0, u, i, x, None, vk._stream, None) is None
+        assert n.cache8_attention(c, 0, u, x, x, i, u, None, True, vk._stream, None) is None

@@ -160,10 +160,12 @@ def test_keys_turned_for_the_packed_cache():
 
 
 def test_tensors_of_another_device_are_refused():
-    """(One device here: the check is asked with a current device that the tensors are not on.)"""
+    """(One device here: the check is asked with a current device that the tensors are not on; the native call layer has the
+    same check, and leaves what fails it to this path.)"""
     s = Server(0, torch.float16)
     q, k, v = s.inputs(1)
     real, vk._cur_device = vk._cur_device, lambda: 1
+    native, vk._native = vk._native, None
     try:
         with pytest.raises(ValueError):
             vk.rotary(s.plan, s.positions(1), q, torch.empty_like(q))
@@ -174,4 +176,29 @@ def test_tensors_of_another_device_are_refused():
         with pytest.raises(ValueError):
             vk.cache8_attention(s.p, 0, s.buf, q, torch.empty_like(q), s.length, s.ws)
     finally:
-        vk._cur_device = real
+        vk._cur_device, vk._native = real, native
+
+
+def test_the_same_with_and_without_the_native_call_layer():
+    assert vk._native is not None
+    outs = []
+    native = vk._native
+    for layer in (native, None):
+        vk._native = layer
+        try:
+            s = Server(1, torch.bfloat16, seed=35)
+            q, k, v = s.inputs(50)
+            pos, out, qt = s.positions(50), torch.empty_like(q), torch.empty_like(q)
+            kt = torch.empty((B, H, 50, 128), dtype=s.dtype, device=DEV)
+            vk.rotary(s.plan, pos, q, qt, k, kt, inverse=True)
+            vk.rotary(s.plan, pos, None, None, kt, kt)
+            s.step(q, k, v, pos, out, qt, i32([50, 0, 49]), i32([50, 0, 49]))
+            vk.cache8_attention(s.p, 0, s.buf, qt, out, i32([50, 0, 49]), s.ws, causal=False)
+            back = torch.empty((B, H, 50, 128), device=DEV)
+            vk.cache8_read(s.p, 0, s.buf, i32([0, 1, 2]), None, back)
+            torch.cuda.synchronize()
+            outs.append((qt, kt, out, back[:, :, :40], s.buf.clone()))
+        finally:
+            vk._native = native
+    for a, b in zip(*outs):
+        assert torch.equal(a.nan_to_num(7.0) if a.is_floating_point() else a, b.nan_to_num(7.0) if b.is_floating_point() else b)
