@@ -81,28 +81,38 @@ inline Rot make_rot(const vidkv_rotary* r, const int32_t* pos, long long rows) {
 // ---- element types --------------------------------------------------------------------------
 typedef float f8v __attribute__((ext_vector_type(8)));
 
+// (Run: 16 bytes as they lie in memory)
 struct TF16 {
   static constexpr int BYTES = 2;
+  typedef h8 Run;
+  static __device__ __forceinline__ Run load(const void* p) { return *static_cast<const h8*>(p); }
+  static __device__ __forceinline__ f8v widen(Run v) { return __builtin_convertvector(v, f8v); }
+  static __device__ __forceinline__ void store(void* p, f8v v) { store8(p, v); }
   static __device__ __forceinline__ f8v load8(const void* p) {
     const h8 v = *static_cast<const h8*>(p);
     return __builtin_convertvector(v, f8v);
   }
   static __device__ __forceinline__ void store8(void* p, f8v v) { *static_cast<h8*>(p) = __builtin_convertvector(v, h8); }
-  static __device__ __forceinline__ f2 load2(const void* p) {
-    const h2 v = *static_cast<const h2*>(p);
+  static __device__ __forceinline__ f2 widen2(uint32_t u) {
+    const h2 v = bits_h2(u);
     return f2{(float)v[0], (float)v[1]};
   }
   static __device__ __forceinline__ void store2(void* p, float a, float b) {
     *static_cast<h2*>(p) = h2{(_Float16)a, (_Float16)b};
   }
-  static __device__ __forceinline__ float round(float x) { return (float)(_Float16)x; }
+  static __device__ __forceinline__ u32x4 pack8(f8v v) { return __builtin_bit_cast(u32x4, __builtin_convertvector(v, h8)); }
+  static __device__ __forceinline__ float of_bits(uint32_t u) { return (float)__builtin_bit_cast(_Float16, (uint16_t)u); }
+  static constexpr float MOST = 65504.0f;
 };
 
 struct TBF16 {
   typedef __bf16 b2 __attribute__((ext_vector_type(2)));
   static constexpr int BYTES = 2;
-  static __device__ __forceinline__ f8v load8(const void* p) {
-    const u32x4 u = *static_cast<const u32x4*>(p);
+  typedef u32x4 Run;
+  static __device__ __forceinline__ Run load(const void* p) { return *static_cast<const u32x4*>(p); }
+  static __device__ __forceinline__ void store(void* p, f8v v) { store8(p, v); }
+  static __device__ __forceinline__ f8v load8(const void* p) { return widen(load(p)); }
+  static __device__ __forceinline__ f8v widen(Run u) {
     f8v r;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -112,18 +122,23 @@ struct TBF16 {
     return r;
   }
   static __device__ __forceinline__ void store8(void* p, f8v v) { *static_cast<b8*>(p) = __builtin_convertvector(v, b8); }
-  static __device__ __forceinline__ f2 load2(const void* p) {
-    const uint32_t u = *static_cast<const uint32_t*>(p);
+  static __device__ __forceinline__ f2 widen2(uint32_t u) {
     return f2{__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u)};
   }
   static __device__ __forceinline__ void store2(void* p, float a, float b) {
     *static_cast<b2*>(p) = b2{(__bf16)a, (__bf16)b};
   }
-  static __device__ __forceinline__ float round(float x) { return (float)(__bf16)x; }
+  static __device__ __forceinline__ u32x4 pack8(f8v v) { return __builtin_bit_cast(u32x4, __builtin_convertvector(v, b8)); }
+  static __device__ __forceinline__ float of_bits(uint32_t u) { return __uint_as_float(u << 16); }
+  static constexpr float MOST = 3.39e38f;
 };
 
 struct TF32 {
   static constexpr int BYTES = 4;
+  typedef f4 Run;
+  static __device__ __forceinline__ Run load(const void* p) { return *static_cast<const f4*>(p); }
+  static __device__ __forceinline__ f4 widen(Run v) { return v; }
+  static __device__ __forceinline__ void store(void* p, f4 v) { *static_cast<f4*>(p) = v; }
   static __device__ __forceinline__ f8v load8(const void* p) {
     const f4 a = static_cast<const f4*>(p)[0], b = static_cast<const f4*>(p)[1];
     return f8v{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
@@ -170,16 +185,21 @@ __device__ __forceinline__ float units(float x, float up, float A, float rA) {
   return fmaf(fmaf(-q, A, n), rA, q);
 }
 
-// Four values in the code's units as four codes.
-template <int CODE>
+// Four values in the code's units as four codes; CLAMP: where a value may be beyond the largest code (a magnitude that was
+// held at its upper bound, which fp16 does not reach).  int8: 1.5 * 2^23 added, which rounds to an integer, ties to even, and
+// leaves it in the low byte.
+template <int CODE, bool CLAMP>
 __device__ __forceinline__ uint32_t code4(float a, float b, float c, float d) {
   constexpr float M = kLevel<CODE>;
-  a = fminf(fmaxf(a, -M), M); b = fminf(fmaxf(b, -M), M);
-  c = fminf(fmaxf(c, -M), M); d = fminf(fmaxf(d, -M), M);
+  if constexpr (CLAMP) {
+    a = __builtin_amdgcn_fmed3f(a, -M, M); b = __builtin_amdgcn_fmed3f(b, -M, M);
+    c = __builtin_amdgcn_fmed3f(c, -M, M); d = __builtin_amdgcn_fmed3f(d, -M, M);
+  }
   if constexpr (CODE == 0) {
-    const uint32_t ia = (uint32_t)(int)rintf(a), ib = (uint32_t)(int)rintf(b);
-    const uint32_t ic = (uint32_t)(int)rintf(c), id = (uint32_t)(int)rintf(d);
-    return (ia & 255u) | (ib & 255u) << 8 | (ic & 255u) << 16 | id << 24;
+    constexpr float R = 12582912.0f;
+    const uint32_t lo = __builtin_amdgcn_perm(__float_as_uint(b + R), __float_as_uint(a + R), 0x0c0c0400u);
+    const uint32_t hi = __builtin_amdgcn_perm(__float_as_uint(d + R), __float_as_uint(c + R), 0x04000c0cu);
+    return lo | hi;
   } else {
     int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);

@@ -16,30 +16,46 @@ struct C8Write {
   uint8_t* vc;
   float* km;
   float* vm;
-  int H, nbc, cap;
+  int H, nbc, cap, n_axes;
   Rot rot;
 };
 
-// Lane maximum of non-negative numbers over the wave.
-__device__ __forceinline__ float wave_max(float v) {
-  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-  r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-#pragma unroll
-  for (int m = 8; m; m >>= 1) v = fmaxf(v, __shfl_xor(v, m));
-  return v;
+typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+
+// Two maxima over the wave at once, each of 16 bits.
+template <int CTRL>
+__device__ __forceinline__ us2 max_dpp(us2 v) {
+  const int u = __builtin_bit_cast(int, v);
+  return __builtin_elementwise_max(v, __builtin_bit_cast(us2, __builtin_amdgcn_update_dpp(u, u, CTRL, 0xf, 0xf, true)));
+}
+__device__ __forceinline__ us2 wave_max(us2 v) {
+  v = max_dpp<0x128>(max_dpp<0x124>(max_dpp<0x122>(max_dpp<0x121>(v))));      // row_ror 1, 2, 4, 8: a row of sixteen
+  // (the elements through integers of their own: a bit cast of a vector's element takes the first one)
+  auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+  uint32_t r0 = r[0], r1 = r[1];
+  v = __builtin_elementwise_max(__builtin_bit_cast(us2, r0), __builtin_bit_cast(us2, r1));
+  r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+  r0 = r[0]; r1 = r[1];
+  return __builtin_elementwise_max(__builtin_bit_cast(us2, r0), __builtin_bit_cast(us2, r1));
 }
 
 // A block's magnitude as it is stored: never zero, and bounded so that no product with it leaves float's range.
 __device__ __forceinline__ float bounded(float a) { return fminf(fmaxf(a, C8_LEAST), C8_MOST); }
 
+// The lane eight further on in its row of sixteen.
+__device__ __forceinline__ uint32_t lane_xor8(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xf, 0xf, true);      // row_ror:8
+}
+
 // One workgroup per block that new tokens reach.  K: thread = 16 channels of one token (two runs of eight, the two
 // sides of eight pairs where the keys are turned); V: wave = lane group kb of the record, lane = two channels of its eight
-// tokens, so that its codes are whole 8-byte pieces of the record.  grid (blocks a sequence can reach, H, B).
+// tokens, so that its codes are whole 8-byte pieces of the record, and two lanes' four pieces two whole 16-byte ones.
+// What a workgroup waits for - rows, positions, a begun block's magnitudes and codes - is asked for as soon as its block
+// is known.  grid (blocks a sequence can reach, H, B).
 template <class T, int CODE, bool ROT>
 __global__ __launch_bounds__(256) void c8_write_kernel(C8Write a) {
-  const int b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int start = a.start[b];
   const int count = a.count ? min(a.count[b], a.n) : a.n;
   if (start < 0 || count <= 0) return;
@@ -50,9 +66,9 @@ __global__ __launch_bounds__(256) void c8_write_kernel(C8Write a) {
   const int lo = max(start, t0), hi = (int)min(min(end, (long long)t0 + G), (long long)a.cap);
   const size_t blk = ((size_t)b * a.H + h) * a.nbc + t0 / G;
   const bool begun = t0 < start;           // live tokens stand before the new ones
-  uint8_t* kc = a.kc + blk * C8REC;
-  uint8_t* vc = a.vc + blk * C8REC;
+  const bool whole = lo == t0 && hi == t0 + G;
   constexpr float LV = kLevel<CODE>;
+  constexpr bool CLAMP = T::MOST > C8_MOST;
 
   // keys
   const int kt = t0 + (tid >> 3), u = tid & 7;
@@ -60,126 +76,143 @@ __global__ __launch_bounds__(256) void c8_write_kernel(C8Write a) {
   int c0 = 16 * u, c1 = c0 + 8;
   const bool turns = ROT && u < a.rot.rot_dim / 16;
   if (turns && !a.rot.adjacent) { c0 = 8 * u; c1 = c0 + a.rot.rot_dim / 2; }
-  f8v x = f8v(0.0f), y = f8v(0.0f);
+  uint2* pk0 = reinterpret_cast<uint2*>(a.kc + blk * C8REC + (tid >> 3) * D + c0);
+  uint2* pk1 = reinterpret_cast<uint2*>(a.kc + blk * C8REC + (tid >> 3) * D + c1);
+  // values: this lane's 16 bytes of the record, channels cv and cv + 16 of lane group w
+  const int cv = (lane >> 4) * 32 + 2 * (lane & 7) + ((lane >> 3) & 1);
+  u32x4* pv = reinterpret_cast<u32x4*>(a.vc + blk * C8REC + (((lane >> 4) * 4 + w) * 16 + (cv & 15)) * 16);
+  typename T::Run rx{}, ry{};
   if (knew) {
     const char* in = a.K.data + b * a.K.sb + h * a.K.sh + (long long)(kt - start) * a.K.st;
-    x = T::load8(in + 2 * c0);
-    y = T::load8(in + 2 * c1);
+    rx = T::load(in + 2 * c0);
+    ry = T::load(in + 2 * c1);
   }
-  // values
-  const char* vin = a.V.data + b * a.V.sb + h * a.V.sh + 4 * lane;
-  f2 v[8];
+  const char* vin = a.V.data + b * a.V.sb + h * a.V.sh;        // (row addresses are the wave's: scalar)
+  uint32_t v[8];                           // two channels of a token, as they lie in memory
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     const int t = t0 + slot_token(w, j);
-    v[j] = (t >= lo && t < hi) ? T::load2(vin + (long long)(t - start) * a.V.st) : f2{0.0f, 0.0f};
+    v[j] = 0;
+    if (whole || (t >= lo && t < hi)) v[j] = *reinterpret_cast<const uint32_t*>(vin + (long long)(t - start) * a.V.st + 4 * lane);
   }
   float ko = 0.0f, vo = 0.0f;
-  if (begun) { ko = bounded(a.km[blk]); vo = bounded(a.vm[blk]); }
+  uint2 k0{}, k1{};
+  u32x4 vold{};
+  if (begun) {
+    ko = a.km[blk]; vo = a.vm[blk];
+    k0 = *pk0; k1 = *pk1;
+  }
+  if (!whole) vold = *pv;
+  int pos[4] = {0, 0, 0, 0};
+  if constexpr (ROT) {
+    const long long row = (long long)b * a.n + (knew ? kt - start : 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) pos[i] = a.rot.pos[min(i, a.n_axes - 1) * a.rot.rows + row];
+  }
+  ko = bounded(ko); vo = bounded(vo);
+  f8v x = T::widen(rx), y = T::widen(ry);
   if constexpr (ROT) {
     if (turns && knew) {
-      const long long row = (long long)b * a.n + (kt - start);
       float co[8], si[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const int i = 8 * u + e;
-        turn_cos_sin(a.rot.pos[(long long)a.rot.axis[i] * a.rot.rows + row], a.rot.turn[i], &co[e], &si[e]);
+        const int ax = a.rot.axis[8 * u + e];
+        turn_cos_sin(ax & 2 ? (ax & 1 ? pos[3] : pos[2]) : (ax & 1 ? pos[1] : pos[0]), a.rot.turn[8 * u + e], &co[e], &si[e]);
       }
-      // (rounded to the tensor's type, as the rotation by itself leaves them)
       if (a.rot.adjacent) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float x1 = x[2 * e], x2 = x[2 * e + 1], y1 = y[2 * e], y2 = y[2 * e + 1];
-          x[2 * e] = T::round(x1 * co[e] - x2 * si[e]);
-          x[2 * e + 1] = T::round(x2 * co[e] + x1 * si[e]);
-          y[2 * e] = T::round(y1 * co[4 + e] - y2 * si[4 + e]);
-          y[2 * e + 1] = T::round(y2 * co[4 + e] + y1 * si[4 + e]);
+          x[2 * e] = x1 * co[e] - x2 * si[e];
+          x[2 * e + 1] = x2 * co[e] + x1 * si[e];
+          y[2 * e] = y1 * co[4 + e] - y2 * si[4 + e];
+          y[2 * e + 1] = y2 * co[4 + e] + y1 * si[4 + e];
         }
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float x1 = x[e], x2 = y[e];
-          x[e] = T::round(x1 * co[e] - x2 * si[e]);
-          y[e] = T::round(x2 * co[e] + x1 * si[e]);
+          x[e] = x1 * co[e] - x2 * si[e];
+          y[e] = x2 * co[e] + x1 * si[e];
         }
       }
     }
   }
 
-  float ka = 0.0f, va = 0.0f;
+  // magnitudes of 16-bit numbers compare as integers do, two at a time
+  us2 vm{0, 0}, km{0, 0};
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    ka = fmaxf(ka, fmaxf(fabsf(x[e]), fabsf(y[e])));
-    va = fmaxf(va, fmaxf(fabsf(v[e][0]), fabsf(v[e][1])));
+  for (int j = 0; j < 8; ++j) vm = __builtin_elementwise_max(vm, __builtin_bit_cast(us2, v[j] & 0x7fff7fffu));
+  u32x4 bx = __builtin_bit_cast(u32x4, rx), by = __builtin_bit_cast(u32x4, ry);
+  if constexpr (ROT) {                     // rounded to the tensor's type, as the rotation by itself leaves them
+    bx = T::pack8(x); by = T::pack8(y);
+    x = T::widen(__builtin_bit_cast(typename T::Run, bx));
+    y = T::widen(__builtin_bit_cast(typename T::Run, by));
   }
-  ka = wave_max(ka);
-  va = wave_max(va);
-  __shared__ float red[2][4];
-  if (lane == 0) { red[0][w] = ka; red[1][w] = va; }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    km = __builtin_elementwise_max(km, __builtin_elementwise_max(__builtin_bit_cast(us2, bx[e] & 0x7fff7fffu),
+                                                                 __builtin_bit_cast(us2, by[e] & 0x7fff7fffu)));
+  us2 most = wave_max(us2{max(km[0], km[1]), max(vm[0], vm[1])});
+  __shared__ us2 red[4];
+  if (lane == 0) red[w] = most;
   __syncthreads();
-  ka = bounded(fmaxf(fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3])), ko));
-  va = bounded(fmaxf(fmaxf(fmaxf(red[1][0], red[1][1]), fmaxf(red[1][2], red[1][3])), vo));
+  most = __builtin_elementwise_max(__builtin_elementwise_max(red[0], red[1]), __builtin_elementwise_max(red[2], red[3]));
+  float ka = bounded(T::of_bits(most[0])), va = bounded(T::of_bits(most[1]));
+  if (begun) { ka = fmaxf(ka, ko); va = fmaxf(va, vo); }
   const float rk = __builtin_amdgcn_rcpf(ka), rv = __builtin_amdgcn_rcpf(va);
   if (tid == 0) { a.km[blk] = ka; a.vm[blk] = va; }
 
-  uint2* pk0 = reinterpret_cast<uint2*>(kc + (tid >> 3) * D + c0);
-  uint2* pk1 = reinterpret_cast<uint2*>(kc + (tid >> 3) * D + c1);
+  // a live token's codes under the new magnitude
+  auto again = [](uint32_t c, float old, float A, float rA) {
+    h2 l, g;
+    decode4<CODE>(c, &l, &g);
+    return code4<CODE, false>(units((float)l[0], old, A, rA), units((float)l[1], old, A, rA), units((float)g[0], old, A, rA),
+                       units((float)g[1], old, A, rA));
+  };
   if (knew) {
     uint2 p, q;
-    p.x = code4<CODE>(units(x[0], LV, ka, rk), units(x[1], LV, ka, rk), units(x[2], LV, ka, rk), units(x[3], LV, ka, rk));
-    p.y = code4<CODE>(units(x[4], LV, ka, rk), units(x[5], LV, ka, rk), units(x[6], LV, ka, rk), units(x[7], LV, ka, rk));
-    q.x = code4<CODE>(units(y[0], LV, ka, rk), units(y[1], LV, ka, rk), units(y[2], LV, ka, rk), units(y[3], LV, ka, rk));
-    q.y = code4<CODE>(units(y[4], LV, ka, rk), units(y[5], LV, ka, rk), units(y[6], LV, ka, rk), units(y[7], LV, ka, rk));
+    p.x = code4<CODE, CLAMP>(units(x[0], LV, ka, rk), units(x[1], LV, ka, rk), units(x[2], LV, ka, rk), units(x[3], LV, ka, rk));
+    p.y = code4<CODE, CLAMP>(units(x[4], LV, ka, rk), units(x[5], LV, ka, rk), units(x[6], LV, ka, rk), units(x[7], LV, ka, rk));
+    q.x = code4<CODE, CLAMP>(units(y[0], LV, ka, rk), units(y[1], LV, ka, rk), units(y[2], LV, ka, rk), units(y[3], LV, ka, rk));
+    q.y = code4<CODE, CLAMP>(units(y[4], LV, ka, rk), units(y[5], LV, ka, rk), units(y[6], LV, ka, rk), units(y[7], LV, ka, rk));
     *pk0 = p;
     *pk1 = q;
-  } else if (kt < start && ka > ko) {      // (only in a begun block) live tokens under the new magnitude
-    auto again = [&](uint32_t c) {
-      h2 l, g;
-      decode4<CODE>(c, &l, &g);
-      return code4<CODE>(units((float)l[0], ko, ka, rk), units((float)l[1], ko, ka, rk), units((float)g[0], ko, ka, rk),
-                         units((float)g[1], ko, ka, rk));
-    };
-    const uint2 p = *pk0, q = *pk1;
-    *pk0 = uint2{again(p.x), again(p.y)};
-    *pk1 = uint2{again(q.x), again(q.y)};
+  } else if (kt < start && ka > ko) {      // (only in a begun block)
+    *pk0 = uint2{again(k0.x, ko, ka, rk), again(k0.y, ko, ka, rk)};
+    *pk1 = uint2{again(k1.x, ko, ka, rk), again(k1.y, ko, ka, rk)};
   }
 
-  // the record's bytes of channel 2 lane + i, lane group w
-  const bool whole = lo == t0 && hi == t0 + G;
+  // the codes of channels 2 lane and 2 lane + 1; channel and channel + 16 go into one piece: lanes 0..7 of a row of 16 take
+  // the even channels of both, lanes 8..15 the odd ones
+  uint2 n[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const int c = 2 * lane + i;
-    uint2* pv = reinterpret_cast<uint2*>(vc + (((c >> 5) * 4 + w) * 16 + (c & 15)) * 16 + ((c >> 4) & 1) * 8);
-    uint2 n;
-    n.x = code4<CODE>(units(v[0][i], LV, va, rv), units(v[1][i], LV, va, rv), units(v[2][i], LV, va, rv),
-                      units(v[3][i], LV, va, rv));
-    n.y = code4<CODE>(units(v[4][i], LV, va, rv), units(v[5][i], LV, va, rv), units(v[6][i], LV, va, rv),
-                      units(v[7][i], LV, va, rv));
-    if (!whole) {
-      const uint2 o = *pv;
-      uint2 m = o;                                            // live tokens' codes
-      if (begun && va > vo) {
-        h2 l, g;
-        decode4<CODE>(o.x, &l, &g);
-        m.x = code4<CODE>(units((float)l[0], vo, va, rv), units((float)l[1], vo, va, rv), units((float)g[0], vo, va, rv),
-                          units((float)g[1], vo, va, rv));
-        decode4<CODE>(o.y, &l, &g);
-        m.y = code4<CODE>(units((float)l[0], vo, va, rv), units((float)l[1], vo, va, rv), units((float)g[0], vo, va, rv),
-                          units((float)g[1], vo, va, rv));
-      }
-      auto pick = [&](uint32_t neu, uint32_t live, uint32_t old, int j0) {
-        uint32_t r = 0;
+    float f[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int t = t0 + slot_token(w, j0 + j);
-          r |= (t >= lo && t < hi ? neu : t < start ? live : old) & (255u << (8 * j));
-        }
-        return r;
-      };
-      n = uint2{pick(n.x, m.x, o.x, 0), pick(n.y, m.y, o.y, 4)};
-    }
-    *pv = n;
+    for (int j = 0; j < 8; ++j) f[j] = units(T::widen2(v[j])[i], LV, va, rv);
+    n[i] = uint2{code4<CODE, CLAMP>(f[0], f[1], f[2], f[3]), code4<CODE, CLAMP>(f[4], f[5], f[6], f[7])};
   }
+  const bool upper = lane & 8;
+  const uint2 give = upper ? n[0] : n[1], keep = upper ? n[1] : n[0];
+  const uint2 got{lane_xor8(give.x), lane_xor8(give.y)};
+  u32x4 r = upper ? u32x4{got.x, got.y, keep.x, keep.y} : u32x4{keep.x, keep.y, got.x, got.y};
+  if (!whole) {
+    uint32_t fresh[2] = {0, 0}, live[2] = {0, 0};              // the bytes of new and of live tokens
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int t = t0 + slot_token(w, j);
+      if (t >= lo && t < hi) fresh[j >> 2] |= 255u << (8 * (j & 3));
+      else if (t < start) live[j >> 2] |= 255u << (8 * (j & 3));
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t o = vold[i];
+      if (begun && va > vo) o = (again(o, vo, va, rv) & live[i & 1]) | (o & ~live[i & 1]);
+      r[i] = (r[i] & fresh[i & 1]) | (o & ~fresh[i & 1]);
+    }
+  }
+  *pv = r;
 }
 
 hipError_t launch_c8_write(const C8Geom& g, int layer, int n, const vidkv_view* K, const vidkv_view* V,
@@ -195,6 +228,7 @@ hipError_t launch_c8_write(const C8Geom& g, int layer, int n, const vidkv_view* 
   a.vm = reinterpret_cast<float*>(cache + g.v_mag) + blk0;
   a.H = g.H; a.nbc = g.nbc; a.cap = g.cap;
   a.rot = make_rot(rot, pos, (long long)g.B * n);
+  a.n_axes = rot ? rot->n_axes : 1;
   // tokens that do not fit are dropped: no more blocks than the cache has
   const long long reach = ((long long)n + 2 * G - 2) / G;
   const dim3 grid((unsigned)(reach < g.nbc ? reach : g.nbc), g.H, g.B), blk(256);

@@ -237,58 +237,61 @@ __device__ __forceinline__ void put_out(const C8Attn& a, int b, int h, int row, 
 
 // Waves share out the blocks of a split, for up to 16 NT rows a KV head.  grid (splits, H, B).
 template <int NT, int CODE>
-__global__ __launch_bounds__(256) void c8_few_kernel(C8Attn a) {
+__global__ __launch_bounds__(256, NT < 3 ? 2 : 1) void c8_few_kernel(C8Attn a) {
   const int b = blockIdx.z, h = blockIdx.y, sp = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int x = lane & 15, kb = lane >> 4;
   const int len = min(max(a.length[b], 0), a.cap);
   const int nq = a.q_count ? min(max(a.q_count[b], 0), a.n) : a.n;
   const int rows = a.n * a.rep;
-  Rows<NT> r;
-  load_rows<NT>(r, a, b, h, 0, rows, len, nq, lane);
   const int nb = (len + G - 1) / G, units = 4 * a.splits, un = 4 * sp + w;
   const int b0 = (int)((long long)un * nb / units), b1 = (int)((long long)(un + 1) * nb / units);
   const int all = a.causal ? max(len - nq + 1, 0) : len;          // tokens that every row sees
   const size_t head = ((size_t)b * a.H + h) * a.nbc;
+  Rows<NT> r;
+  Block f, g;
+  if (b0 < b1) load_block(f, a.kc, a.vc, a.km, a.vm, head + b0, lane);      // (on its way while the queries are laid out)
+  load_rows<NT>(r, a, b, h, 0, rows, len, nq, lane);
   if (b0 < b1) {
-    Block f, g;
-    load_block(f, a.kc, a.vc, a.km, a.vm, head + b0, lane);
     for (int i = b0; i < b1; ++i) {
       if (i + 1 < b1) load_block(g, a.kc, a.vc, a.km, a.vm, head + i + 1, lane);
       take_codes<NT, CODE>(r, f, (i + 1) * G > all, i * G, len, lane);
       f = g;
     }
   }
-  // the four waves' sums
-  __shared__ f4 so[4][NT * 16][D / 4 + 1];
-  __shared__ float sm[4][NT * 16], sl[4][NT * 16];
+  // the four waves' sums, a tile of rows at a time
+  __shared__ f4 so[4][16][D / 4 + 1];
+  __shared__ float sm[4][16], sl[4][16];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const float l = row_sum(r, t);
-    if (kb == 0) { sm[w][16 * t + x] = r.m[t]; sl[w][16 * t + x] = l; }
+    if (t > 0) __syncthreads();
+    if (kb == 0) { sm[w][x] = r.m[t]; sl[w][x] = l; }
 #pragma unroll
-    for (int m = 0; m < 8; ++m) so[w][16 * t + x][4 * m + kb] = r.o[t][m];
-  }
-  __syncthreads();
-  for (int e = tid; e < rows * (D / 4); e += 256) {
-    const int row = e / (D / 4), c4 = e - row * (D / 4);
-    float M = NONE;
+    for (int m = 0; m < 8; ++m) so[w][x][4 * m + kb] = r.o[t][m];
+    __syncthreads();
 #pragma unroll
-    for (int k = 0; k < 4; ++k) M = fmaxf(M, sm[k][row]);
-    f4 o = f4{0.f, 0.f, 0.f, 0.f};
-    float l = 0.0f;
+    for (int e = tid; e < 16 * (D / 4); e += 256) {
+      const int rr = e / (D / 4), c4 = e % (D / 4), row = 16 * t + rr;
+      if (row >= rows) continue;
+      float M = NONE;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float wt = __builtin_amdgcn_exp2f(sm[k][row] - M);
-      o += so[k][row][c4] * wt;
-      l = fmaf(sl[k][row], wt, l);
-    }
-    if (a.po) {
-      const size_t at = (((size_t)b * a.H + h) * rows + row) * a.splits + sp;
-      reinterpret_cast<f4*>(a.po)[at * (D / 4) + c4] = o;
-      if (c4 == 0) { a.pml[2 * at] = M; a.pml[2 * at + 1] = l; }
-    } else {
-      put_out(a, b, h, row, 4 * c4, l != 0.0f ? o * (a.inv_level / l) : f4{0.f, 0.f, 0.f, 0.f});
+      for (int k = 0; k < 4; ++k) M = fmaxf(M, sm[k][rr]);
+      f4 o = f4{0.f, 0.f, 0.f, 0.f};
+      float l = 0.0f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float wt = __builtin_amdgcn_exp2f(sm[k][rr] - M);
+        o += so[k][rr][c4] * wt;
+        l = fmaf(sl[k][rr], wt, l);
+      }
+      if (a.po) {
+        const size_t at = (((size_t)b * a.H + h) * rows + row) * a.splits + sp;
+        reinterpret_cast<f4*>(a.po)[at * (D / 4) + c4] = o;
+        if (c4 == 0) { a.pml[2 * at] = M; a.pml[2 * at + 1] = l; }
+      } else {
+        put_out(a, b, h, row, 4 * c4, l != 0.0f ? o * (a.inv_level / l) : f4{0.f, 0.f, 0.f, 0.f});
+      }
     }
   }
 }
@@ -546,6 +549,9 @@ __global__ __launch_bounds__(256) void c8_merge_kernel(C8Attn a) {
       ml[u] = pm[s];
       v[u] = po[(size_t)s * (D / 4)];
     }
+    // (left to itself the compiler waits for (m, l) first, and for the sums only behind the maximum)
+#pragma unroll
+    for (int u = 0; u < 8; ++u) asm volatile("" : "+v"(v[u]), "+v"(ml[u]));
     float top = M;
 #pragma unroll
     for (int u = 0; u < 8; ++u) top = fmaxf(top, ml[u][0]);
@@ -592,12 +598,14 @@ struct C8Plan {
 static C8Plan c8_plan(const C8Geom& g, int n) {
   C8Plan p{};
   const long long rows = (long long)n * g.rep;
-  p.few = rows <= 32;
-  p.nt = !p.few ? 3 : rows <= 16 ? 1 : 2;
+  p.few = rows <= 48;
+  p.nt = !p.few ? 3 : (int)(rows + 15) / 16;
   p.tiles = p.few ? 1 : (int)((rows + 64 * p.nt - 1) / (64 * p.nt));
   // two workgroups a compute unit; four where waves share blocks and the sequences' lengths can differ (one layer of 64
-  // sequences of 12544 to 25088 tokens: 170 us with two, 160 with four; one of 196000: 39.0 and 39.8, the merge 4.1 and 5.9)
-  const long long wgs = (long long)p.tiles * g.H * g.B, want = (p.few && g.B > 1 ? 4LL : 2LL) * device_cu_count();
+  // sequences of 12544 to 25088 tokens: 170 us with two, 160 with four; one of 196000: 39.0 and 39.8, the merge 4.1 and 5.9);
+  // one where three tiles of rows leave room for one (40 rows, 16 sequences of up to 6001 tokens: 21.6 us, with two 23.9)
+  const long long wgs = (long long)p.tiles * g.H * g.B;
+  const long long want = (!p.few ? 2LL : p.nt == 3 ? 1LL : g.B > 1 ? 4LL : 2LL) * device_cu_count();
   long long s = (want + wgs - 1) / wgs;
   const long long most = p.few ? (g.nbc + 3) / 4 : (g.nbc + 7) / 8;
   p.splits = (int)std::max(1LL, std::min({s, most, 256LL}));
@@ -636,15 +644,22 @@ hipError_t launch_c8_attn(const C8Geom& g, int layer, int n, int causal, float s
     constexpr int CODE = decltype(code)::value;
     const dim3 few(p.splits, g.H, g.B);
     if (p.few && p.nt == 1) hipLaunchKernelGGL((c8_few_kernel<1, CODE>), few, blk, 0, st, a);
-    else if (p.few) hipLaunchKernelGGL((c8_few_kernel<2, CODE>), few, blk, 0, st, a);
+    else if (p.few && p.nt == 2) hipLaunchKernelGGL((c8_few_kernel<2, CODE>), few, blk, 0, st, a);
+    else if (p.few) hipLaunchKernelGGL((c8_few_kernel<3, CODE>), few, blk, 0, st, a);
     else hipLaunchKernelGGL((c8_many_kernel<3, CODE>), dim3(p.tiles * p.splits * g.H * g.B), blk, 0, st, a, p.tiles);
   };
   if (g.code == 0) by_code(std::integral_constant<int, 0>{});
   else by_code(std::integral_constant<int, 1>{});
   if (a.po) {
     const int rows = n * g.rep;
-    if (p.splits > 8) hipLaunchKernelGGL(c8_merge_kernel<8>, dim3(rows, g.H, g.B), blk, 0, st, a);
-    else hipLaunchKernelGGL(c8_merge_kernel<1>, dim3((rows + 7) / 8, g.H, g.B), blk, 0, st, a);
+    auto merge = [&](auto sl) {
+      constexpr int SL = decltype(sl)::value;
+      hipLaunchKernelGGL(c8_merge_kernel<SL>, dim3((rows + 8 / SL - 1) / (8 / SL), g.H, g.B), blk, 0, st, a);
+    };
+    if (p.splits > 32) merge(std::integral_constant<int, 8>{});
+    else if (p.splits > 16) merge(std::integral_constant<int, 4>{});
+    else if (p.splits > 8) merge(std::integral_constant<int, 2>{});
+    else merge(std::integral_constant<int, 1>{});
   }
   return hipGetLastError();
 }

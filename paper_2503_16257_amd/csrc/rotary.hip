@@ -2,7 +2,7 @@
 //   y1 = x1 cos - x2 sin,  y2 = x2 cos + x1 sin,
 // forward and inverse (the backward pass).  2 x the element's bytes of traffic an element and about four
 // operations: bound by HBM, for single tokens by the launch.  cos and sin belong to a (token, pair), not to a head: a thread
-// makes those of eight pairs once and turns them in several heads.
+// makes those of its pairs once and turns them in several heads.
 #include "cache8.h"
 
 namespace vidkv {
@@ -14,62 +14,73 @@ struct RotaryArgs {
   int rows;                    // sequences x tokens
   int per;                     // heads a thread
   float sign;                  // -1: inverse
+  int n_axes;
   Rot rot;
 };
 
-// Thread = 16 channels of one token (a unit) in `per` heads: eight pairs, or 16 channels behind rot_dim.
+// A unit is two runs of 16 bytes of a token's head: the two sides of as many pairs as a run has elements, or 32 bytes
+// behind rot_dim.  Thread = one unit of one token in `per` heads.  What a thread waits for is asked for at once: the pairs'
+// axes and turns, the positions of every axis, the first head's channels.
 // grid (ceil(rows / tokens a workgroup), ceil(heads / per)).
 template <class T>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
-  const int U = a.rot.head_dim / 16, tpw = 256 / U;
+  constexpr int E = 16 / T::BYTES;         // elements a run
+  typedef float fe __attribute__((ext_vector_type(E)));
+  const int U = a.rot.head_dim / (2 * E), tpw = 256 / U;
   const int tok = threadIdx.x / U, u = threadIdx.x - tok * U;
   const int row = blockIdx.x * tpw + tok;
   if (tok >= tpw || row >= a.rows) return;
   const int b = row / a.n, t = row - b * a.n;
-  const int ur = a.rot.rot_dim / 16;
-  int c0 = 16 * u, c1 = c0 + 8;            // the two runs of eight channels
-  const bool turns = u < ur;
-  if (turns && !a.rot.adjacent) { c0 = 8 * u; c1 = c0 + a.rot.rot_dim / 2; }
-  float co[8], si[8];
+  int c0 = 2 * E * u, c1 = c0 + E;         // the two runs
+  const bool turns = c0 < a.rot.rot_dim;
+  if (turns && !a.rot.adjacent) { c0 = E * u; c1 = c0 + a.rot.rot_dim / 2; }
+  const int h0 = blockIdx.y * a.per, h1 = min(h0 + a.per, a.Hq + a.Hk);
+  auto at = [&](int h, const View& q, const View& k) {
+    const View& v = h < a.Hq ? q : k;
+    const int hh = h < a.Hq ? h : h - a.Hq;
+    return v.data + b * v.sb + hh * v.sh + t * v.st;
+  };
+  typename T::Run r0 = T::load(at(h0, a.q, a.k) + c0 * T::BYTES), r1 = T::load(at(h0, a.q, a.k) + c1 * T::BYTES);
+  float co[E], si[E];
   if (turns) {
+    int pos[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int i = 8 * u + e;
-      turn_cos_sin(a.rot.pos[(long long)a.rot.axis[i] * a.rows + row], a.rot.turn[i], &co[e], &si[e]);
+    for (int x = 0; x < 4; ++x) pos[x] = a.rot.pos[(long long)min(x, a.n_axes - 1) * a.rows + row];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int ax = a.rot.axis[E * u + e];
+      turn_cos_sin(ax & 2 ? (ax & 1 ? pos[3] : pos[2]) : (ax & 1 ? pos[1] : pos[0]), a.rot.turn[E * u + e], &co[e], &si[e]);
       si[e] *= a.sign;
     }
   }
-  const int h0 = blockIdx.y * a.per, h1 = min(h0 + a.per, a.Hq + a.Hk);
-#pragma unroll 4
   for (int h = h0; h < h1; ++h) {
-    const bool isq = h < a.Hq;
-    const View& vi = isq ? a.q : a.k;
-    const View& vo = isq ? a.qo : a.ko;
-    const int hh = isq ? h : h - a.Hq;
-    const char* in = vi.data + b * vi.sb + hh * vi.sh + t * vi.st;
-    char* out = vo.data + b * vo.sb + hh * vo.sh + t * vo.st;
-    f8v x = T::load8(in + c0 * T::BYTES), y = T::load8(in + c1 * T::BYTES);
+    fe x = T::widen(r0), y = T::widen(r1);
+    if (h + 1 < h1) {                      // the next head's, in flight meanwhile
+      r0 = T::load(at(h + 1, a.q, a.k) + c0 * T::BYTES);
+      r1 = T::load(at(h + 1, a.q, a.k) + c1 * T::BYTES);
+    }
     if (turns) {
       if (a.rot.adjacent) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
+        for (int e = 0; e < E / 2; ++e) {
           const float x1 = x[2 * e], x2 = x[2 * e + 1], y1 = y[2 * e], y2 = y[2 * e + 1];
           x[2 * e] = x1 * co[e] - x2 * si[e];
           x[2 * e + 1] = x2 * co[e] + x1 * si[e];
-          y[2 * e] = y1 * co[4 + e] - y2 * si[4 + e];
-          y[2 * e + 1] = y2 * co[4 + e] + y1 * si[4 + e];
+          y[2 * e] = y1 * co[E / 2 + e] - y2 * si[E / 2 + e];
+          y[2 * e + 1] = y2 * co[E / 2 + e] + y1 * si[E / 2 + e];
         }
       } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < E; ++e) {
           const float x1 = x[e], x2 = y[e];
           x[e] = x1 * co[e] - x2 * si[e];
           y[e] = x2 * co[e] + x1 * si[e];
         }
       }
     }
-    T::store8(out + c0 * T::BYTES, x);
-    T::store8(out + c1 * T::BYTES, y);
+    char* out = const_cast<char*>(at(h, a.qo, a.ko));
+    T::store(out + c0 * T::BYTES, x);
+    T::store(out + c1 * T::BYTES, y);
   }
 }
 
@@ -80,8 +91,9 @@ hipError_t launch_rotary(const vidkv_rotary* r, int inverse, int B, int n, const
   a.Hq = q ? Hq : 0; a.Hk = k ? Hk : 0;
   a.n = n; a.rows = B * n;
   a.sign = inverse ? -1.0f : 1.0f;
+  a.n_axes = r->n_axes;
   a.rot = make_rot(r, pos, a.rows);
-  const int heads = a.Hq + a.Hk, tpw = 256 / (r->head_dim / 16);
+  const int heads = a.Hq + a.Hk, tpw = 256 / (r->head_dim * dtype_bytes(dtype) / 32);
   const int tiles = (a.rows + tpw - 1) / tpw;
   a.per = 1;
   while (a.per < 8 && (long long)tiles * ((heads + 2 * a.per - 1) / (2 * a.per)) >= 2048) a.per *= 2;
