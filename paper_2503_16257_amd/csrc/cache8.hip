@@ -54,6 +54,10 @@ __device__ __forceinline__ uint32_t lane_xor8(uint32_t v) {
 // is known.  grid (blocks a sequence can reach, H, B).
 template <class T, int CODE, bool ROT>
 __global__ __launch_bounds__(256) void c8_write_kernel(C8Write a) {
+  // (all arguments in one round trip; left to itself the compiler asks for each where it is used)
+  asm volatile("" :: "s"(a.K.data), "s"(a.K.sb), "s"(a.K.sh), "s"(a.K.st), "s"(a.V.data), "s"(a.V.sb), "s"(a.V.sh), "s"(a.V.st),
+               "s"(a.start), "s"(a.count), "s"(a.kc), "s"(a.vc), "s"(a.km), "s"(a.vm), "s"(a.H), "s"(a.nbc), "s"(a.cap), "s"(a.n));
+  if constexpr (ROT) asm volatile("" :: "s"(a.rot.pos), "s"(a.rot.rows), "s"(a.rot.rot_dim), "s"(a.rot.adjacent), "s"(a.n_axes));
   const int b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int start = a.start[b];

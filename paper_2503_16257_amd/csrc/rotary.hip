@@ -24,6 +24,10 @@ struct RotaryArgs {
 // grid (ceil(rows / tokens a workgroup), ceil(heads / per)).
 template <class T>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
+  // (all arguments in one round trip; left to itself the compiler asks for each where it is used)
+  asm volatile("" :: "s"(a.q.data), "s"(a.q.sb), "s"(a.q.sh), "s"(a.q.st), "s"(a.k.data), "s"(a.k.sb), "s"(a.k.sh), "s"(a.k.st),
+               "s"(a.qo.data), "s"(a.ko.data), "s"(a.Hq), "s"(a.Hk), "s"(a.n), "s"(a.rows), "s"(a.per), "s"(a.rot.pos),
+               "s"(a.rot.head_dim), "s"(a.rot.rot_dim), "s"(a.rot.adjacent), "s"(a.n_axes));
   constexpr int E = 16 / T::BYTES;         // elements a run
   typedef float fe __attribute__((ext_vector_type(E)));
   const int U = a.rot.head_dim / (2 * E), tpw = 256 / U;
