@@ -351,7 +351,8 @@ vidkv_status vidkv_rotary_init(vidkv_rotary *rot, int32_t head_dim, int32_t rot_
  *   k, k_out       : [batch, n_k_heads, ...] likewise, of q's dtype
  *   inverse        : 0 turns by +angle; 1 by -angle: undoes the rotation, and is
  *                    its backward pass (gradients of y in, gradients of x out)
- * Computed in fp32 (angles to 2^-33 turns), rounded once. */
+ * Computed in fp32 (angles to 2^-33 turns), rounded once.  batch * n_tokens is at
+ * most 2^26 (else VIDKV_ESHAPE). */
 vidkv_status vidkv_rotary_apply(const vidkv_rotary *rot, int32_t inverse, int32_t batch,
                                 int32_t n_tokens, const int32_t *pos_dev, int32_t n_q_heads,
                                 const vidkv_view *q, const vidkv_view *q_out, int32_t n_k_heads,
@@ -361,19 +362,21 @@ vidkv_status vidkv_rotary_apply(const vidkv_rotary *rot, int32_t inverse, int32_
  * it holds its magnitude A = max |x|, clamped to 2^-40..2^40, and codes
  *   code 0 (int8): rint(x * 127 / A), value = code * A / 127
  *   code 1 (e4m3): the nearest e4m3 number to x * 448 / A, value = that * A / 448
- * (ties to even in both). */
+ * (ties to even in both; what is not finite gives unspecified codes). */
 typedef struct vidkv_cache8 {
   int32_t n_layers, batch, n_kv_heads;
   int32_t n_q_heads;      /* multiple of n_kv_heads, any ratio                   */
   int32_t head_dim;       /* must be 128                                         */
-  int32_t capacity;       /* tokens a sequence, multiple of 32, >= 32            */
+  int32_t capacity;       /* tokens a sequence, multiple of 32, 32..2^28         */
   int32_t code;           /* 0 int8, 1 e4m3                                      */
   float softmax_scale;    /* multiplies q.k before the softmax, > 0              */
 } vidkv_cache8;
 
 /* Size queries (host): bytes of the cache buffer of all layers, and of the
- * workspace of an attention call of up to n_query queries a sequence; 0 when
- * *p or n_query is invalid.  n_kv_heads and batch at most 65535. */
+ * workspace that is enough for attention calls of up to n_query queries a
+ * sequence; 0 when *p or n_query is invalid.  n_kv_heads and batch at most
+ * 65535; at most 2^28 tokens a call, and 2^28 queries times heads of a group
+ * (VIDKV_ESHAPE). */
 size_t vidkv_cache8_bytes(const vidkv_cache8 *p);
 size_t vidkv_cache8_workspace_bytes(const vidkv_cache8 *p, int32_t n_query);
 

@@ -26,7 +26,7 @@ inline bool make_c8(const vidkv_cache8* p, C8Geom* g) {
   if (!p) return false;
   if (p->n_layers < 1 || p->batch < 1 || p->n_kv_heads < 1 || p->batch > 65535 || p->n_kv_heads > 65535) return false;
   if (p->n_q_heads < p->n_kv_heads || p->n_q_heads % p->n_kv_heads) return false;
-  if (p->head_dim != D || p->capacity < G || p->capacity % G) return false;
+  if (p->head_dim != D || p->capacity < G || p->capacity % G || p->capacity > (1 << 28)) return false;
   if (p->code != 0 && p->code != 1) return false;
   g->L = p->n_layers; g->B = p->batch; g->H = p->n_kv_heads; g->Hq = p->n_q_heads;
   g->rep = g->Hq / g->H;

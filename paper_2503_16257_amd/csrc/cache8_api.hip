@@ -15,6 +15,8 @@ hipError_t launch_c8_attn(const C8Geom& g, int layer, int n, int causal, float s
                           const uint8_t* cache, const int32_t* length, const int32_t* q_count, const vidkv_view* out,
                           void* ws, hipStream_t st);
 size_t c8_attn_ws_bytes(const C8Geom& g, int n);
+size_t c8_attn_ws_need(const C8Geom& g, int n);
+bool c8_attn_fits(const C8Geom& g, int n);
 }  // namespace vidkv
 
 using namespace vidkv;
@@ -42,8 +44,9 @@ bool good_rotary(const vidkv_rotary* r) {
   return true;
 }
 
-// rows x query heads of a call: what the kernels count in 32 bits
-bool few_enough(const C8Geom& g, int n) { return (long long)n * g.rep <= (1 << 30); }
+// Tokens of a call, and rows (queries x heads of a group): HIP counts a grid dimension's threads in 32 bits.
+constexpr int32_t MOST_TOKENS = 1 << 28;
+bool few_enough(const C8Geom& g, int n) { return (long long)n * g.rep <= MOST_TOKENS; }
 }  // namespace
 
 extern "C" {
@@ -84,7 +87,7 @@ vidkv_status vidkv_rotary_apply(const vidkv_rotary* rot, int32_t inverse, int32_
   if (!rot || !pos || (!q && !k) || (q && !q_out) || (k && !k_out)) return VIDKV_EINVAL;
   if (!good_rotary(rot) || (inverse != 0 && inverse != 1) || !at(pos, 4)) return VIDKV_EINVAL;
   if (batch < 0 || n_tokens < 0 || (q && n_q_heads < 0) || (k && n_k_heads < 0)) return VIDKV_EINVAL;
-  if ((int64_t)batch * n_tokens > (1 << 30) || (q && n_q_heads > 65535) || (k && n_k_heads > 65535)) return VIDKV_ESHAPE;
+  if ((int64_t)batch * n_tokens > (1 << 26) || (q && n_q_heads > 65535) || (k && n_k_heads > 65535)) return VIDKV_ESHAPE;
   const long long heads = (q ? n_q_heads : 0) + (k ? n_k_heads : 0);
   if (heads > 65535) return VIDKV_ESHAPE;
   const int32_t dtype = q ? q->dtype : k->dtype;
@@ -114,6 +117,7 @@ vidkv_status vidkv_cache8_write(const vidkv_cache8* p, int32_t layer, int32_t n_
   C8Geom g;
   if (!p || !cache || !start) return VIDKV_EINVAL;
   if (!make_c8(p, &g)) return VIDKV_ESHAPE;
+  if (n_tokens > MOST_TOKENS) return VIDKV_ESHAPE;
   if (layer < 0 || layer >= g.L || n_tokens < 0) return VIDKV_EINVAL;
   if (!good_view(K, false) || !good_view(V, false) || K->dtype != V->dtype) return VIDKV_EINVAL;
   if ((rot != nullptr) != (pos != nullptr)) return VIDKV_EINVAL;
@@ -133,6 +137,7 @@ vidkv_status vidkv_cache8_read(const vidkv_cache8* p, int32_t layer, int32_t n_t
   C8Geom g;
   if (!p || !cache || !start || (!K && !V)) return VIDKV_EINVAL;
   if (!make_c8(p, &g)) return VIDKV_ESHAPE;
+  if (n_tokens > MOST_TOKENS) return VIDKV_ESHAPE;
   if (layer < 0 || layer >= g.L || n_tokens < 0) return VIDKV_EINVAL;
   if ((K && !good_view(K, true)) || (V && !good_view(V, true)) || (K && V && K->dtype != V->dtype)) return VIDKV_EINVAL;
   if (!at(cache, 256) || !at(start, 4)) return VIDKV_EINVAL;
@@ -153,11 +158,11 @@ vidkv_status vidkv_cache8_attention(const vidkv_cache8* p, int32_t layer, int32_
   if (!make_c8(p, &g)) return VIDKV_ESHAPE;
   if (layer < 0 || layer >= g.L || n_query < 0 || (causal != 0 && causal != 1)) return VIDKV_EINVAL;
   if (!(p->softmax_scale > 0.0f) || !(p->softmax_scale < 1e30f)) return VIDKV_EINVAL;
-  if (!few_enough(g, n_query)) return VIDKV_ESHAPE;
+  if (!few_enough(g, n_query) || (n_query > 0 && !c8_attn_fits(g, n_query))) return VIDKV_ESHAPE;
   if (!good_view(q, false) || !good_view(out, false) || q->dtype != out->dtype) return VIDKV_EINVAL;
   if (!at(cache, 256) || !at(ws, 256) || !at(length, 4) || !at(q_count, 4)) return VIDKV_EINVAL;
   if (n_query == 0) return VIDKV_OK;
-  if (cache_bytes < g.total || ws_bytes < c8_attn_ws_bytes(g, n_query)) return VIDKV_ENOSPACE;
+  if (cache_bytes < g.total || ws_bytes < c8_attn_ws_need(g, n_query)) return VIDKV_ENOSPACE;
   if (!stream_on_current_device(static_cast<hipStream_t>(stream))) return VIDKV_EINVAL;
   const hipError_t e = launch_c8_attn(g, layer, n_query, causal, p->softmax_scale, q, static_cast<const uint8_t*>(cache),
                                       length, q_count, out, ws, static_cast<hipStream_t>(stream));

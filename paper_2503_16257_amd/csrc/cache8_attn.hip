@@ -619,10 +619,31 @@ static C8Plan c8_plan(const C8Geom& g, int n) {
   return p;
 }
 
+// Bytes of a call's partials.
+static size_t c8_parts(const C8Geom& g, long long rows, int splits) {
+  return splits > 1 ? align256((size_t)g.B * g.H * rows * splits * (D + 2) * sizeof(float)) : 0;
+}
+size_t c8_attn_ws_need(const C8Geom& g, int n) { return c8_parts(g, (long long)n * g.rep, c8_plan(g, n).splits) + 256; }
+
+// ... and of the largest of the calls of up to n queries: fewer rows can mean more splits.  The plan changes with the
+// tiles of 16 or 192 rows; behind the last tile that is split there are no partials.
 size_t c8_attn_ws_bytes(const C8Geom& g, int n) {
+  size_t most = 0;
+  for (long long q = 1; q <= n;) {
+    const C8Plan p = c8_plan(g, (int)q);
+    if (!p.few && p.splits == 1) break;
+    const long long rows = p.few ? 16LL * p.nt : 64LL * p.nt * p.tiles;          // the last of this plan
+    const long long last = std::max(q, std::min<long long>(n, rows / g.rep));
+    most = std::max(most, c8_parts(g, last * g.rep, p.splits));
+    q = last + 1;
+  }
+  return most + 256;
+}
+
+// Whether a grid holds the call: HIP counts a dimension's threads in 32 bits.
+bool c8_attn_fits(const C8Geom& g, int n) {
   const C8Plan p = c8_plan(g, n);
-  const size_t parts = p.splits > 1 ? (size_t)g.B * g.Hq * n * p.splits : 0;
-  return align256(parts * (D + 2) * sizeof(float)) + 256;
+  return p.few || (long long)p.tiles * p.splits * g.H * g.B < (1 << 24);
 }
 
 hipError_t launch_c8_attn(const C8Geom& g, int layer, int n, int causal, float scale, const vidkv_view* q,

@@ -105,7 +105,7 @@ def test_rotary_apply_refuses():
     assert call(rot=None) == vk.EINVAL and call(pos=None) == vk.EINVAL and call(pos=A + 2) == vk.EINVAL
     assert call(q=None) == vk.EINVAL and call(qo=None) == vk.EINVAL and call(k=view()) == vk.EINVAL
     assert call(inv=2) == vk.EINVAL and call(B=-1) == vk.EINVAL and call(n=-1) == vk.EINVAL and call(hq=-1) == vk.EINVAL
-    assert call(B=1 << 16, n=1 << 16) == vk.ESHAPE and call(hq=65536) == vk.ESHAPE
+    assert call(B=1 << 16, n=1 << 16) == vk.ESHAPE and call(B=1, n=(1 << 26) + 1) == vk.ESHAPE and call(hq=65536) == vk.ESHAPE
     assert call(hq=40000, hk=40000, k=view(), ko=view()) == vk.ESHAPE
     for bad in (view(data=A + 8), view(data=None), view(b=4), view(h=129), view(n=2), view(dtype=3), view(n=1 << 60)):
         assert call(q=bad) == vk.EINVAL and call(qo=bad) == vk.EINVAL
@@ -135,7 +135,17 @@ def test_cache8_sizes():
         assert vk.cache8_workspace_bytes(p, n) >= 256
     assert vk.cache8_workspace_bytes(p, 0) == 0 and vk.cache8_workspace_bytes(p, -1) == 0
     assert vk.cache8_workspace_bytes(p, 2 ** 31 - 1) == 0
+    assert size(cap=2 ** 28) > 0 and size(cap=2 ** 28 + 32) == 0
     assert vk.lib().vidkv_cache8_bytes(None) == 0
+
+
+@pytest.mark.parametrize("B,H,rep,cap", [(1, 4, 7, 98208), (1, 1, 1, 1568), (3, 2, 8, 6016), (64, 4, 7, 25088), (1, 1, 48, 640)])
+def test_a_workspace_for_many_queries_holds_fewer(B, H, rep, cap):
+    """(More rows can mean fewer splits, and smaller partials.)"""
+    p = vk.make_cache8(1, B, H, H * rep, cap)
+    sizes = [vk.cache8_workspace_bytes(p, n) for n in range(1, 400)]
+    assert sizes == sorted(sizes)
+    assert vk.cache8_workspace_bytes(p, 10 ** 6) >= sizes[-1]
 
 
 def test_cache8_calls_refuse():
@@ -173,7 +183,9 @@ def test_cache8_calls_refuse():
     assert attend(length=None) == vk.EINVAL and attend(length=A + 2) == vk.EINVAL and attend(count=A + 2) == vk.EINVAL
     assert attend(causal=2) == vk.EINVAL and attend(ws=None) == vk.EINVAL and attend(ws=A + 16) == vk.EINVAL
     assert attend(wb=vk.cache8_workspace_bytes(p, 2) - 1) == vk.ENOSPACE
-    assert attend(n=2 ** 31 - 1) == vk.ESHAPE
+    assert attend(n=2 ** 31 - 1) == vk.ESHAPE and write(n=2 ** 28 + 1) == vk.ESHAPE and read(n=2 ** 28 + 1) == vk.ESHAPE
+    wide = vk.make_cache8(1, 65535, 65535, 65535, 32)                       # more workgroups than a grid holds
+    assert attend(p=C.byref(wide), n=2 ** 20, cb=1 << 62) == vk.ESHAPE
     for scale in (0.0, -1.0, math.nan, math.inf):
         odd = vk.make_cache8(2, 1, 4, 28, 64, softmax_scale=scale)
         assert attend(p=C.byref(odd)) == vk.EINVAL

@@ -158,6 +158,26 @@ def test_read_back(code, dtype):
         assert torch.equal(only, V)
 
 
+@pytest.mark.parametrize("code", [0, 1])
+def test_every_code_reads_as_its_number(code):
+    """All 256 bytes, at K's and at V's places, under a magnitude of the level itself (value = code) and an odd one."""
+    c = Cache(1, 1, 1, 64, code)
+    nb = 2 * 32 * 128
+    c.buf[:2 * nb] = torch.arange(2 * nb, dtype=torch.int32, device=DEV).mul(37).to(torch.uint8)
+    c.buf[2 * nb:].view(torch.float32)[:2] = torch.tensor([127.0 if code == 0 else 448.0, 3.3], device=DEV)
+    c.buf[2 * nb + 256:].view(torch.float32)[:2] = torch.tensor([127.0 if code == 0 else 448.0, 2.0 ** -40], device=DEV)
+    K, V = torch.empty((1, 1, 64, 128), device=DEV), torch.empty((1, 1, 64, 128), device=DEV)
+    vk.cache8_read(c.p, 0, c.buf, i32([0]), K, V)
+    kc, vc, km, vm = c.state()
+    assert len(np.unique(kc)) == 256 and len(np.unique(vc)) == 256
+    for got, cc, m in ((K, kc, km), (V, vc, vm)):
+        want = O.values(cc[0, 0, 0], m[0, 0, 0], code)
+        got = f64(got)[0, 0]
+        np.testing.assert_array_equal(np.isnan(got), np.isnan(want))
+        ok = ~np.isnan(want)
+        assert (np.abs(got - want)[ok] <= 3 * 2.0 ** -24 * np.abs(want[ok])).all()
+
+
 def test_a_buffer_beyond_32_bit_offsets():
     """8.6 GB: the last layer's last sequence, codes and magnitudes."""
     L, B, H, cap = 4, 8, 8, 131200

@@ -183,6 +183,20 @@ def test_rows_of_unseen_queries_do_not_depend_on_them():
         assert torch.equal(a[0], b[0]) and torch.isnan(b[1]).all()
 
 
+def test_one_workspace_for_every_number_of_queries():
+    """Sized once for the most queries: fewer ones fit, and nothing behind it is written."""
+    p, buf = filled(1, 1, 7, 6272, [6272], 0, 25)
+    size = vk.cache8_workspace_bytes(p, 29)
+    ws = vk.alloc_bytes(size + 4096, DEV)
+    for n in (29, 28, 27, 7, 6, 1):
+        ws.fill_(0x5A)
+        q = queries(1, 7, n, F16, 26 + n)
+        out = torch.empty_like(q)
+        vk.cache8_attention(p, 0, buf, q, out, i32([6272]), ws[:size])
+        check(p, 0, buf, q, out, [6272], rows=[0, n - 1])
+        assert (ws[size:] == 0x5A).all()
+
+
 def test_a_layer_beyond_32_bit_offsets():
     L, B, H, cap = 5, 8, 8, 131200
     p = vk.make_cache8(L, B, H, H * 2, cap, 1)
