@@ -235,16 +235,17 @@ __device__ __forceinline__ void put_out(const C8Attn& a, int b, int h, int row, 
   }
 }
 
-// Waves share out the blocks of a split, for up to 16 NT rows a KV head.  grid (splits, H, B).
-template <int NT, int CODE>
-__global__ __launch_bounds__(256, NT < 3 ? 2 : 1) void c8_few_kernel(C8Attn a) {
+// W waves share out the blocks of a split, for up to 16 NT rows a KV head.  Bound by HBM, 256 bytes a token and KV head;
+// for short sequences by its chain of round trips: arguments, length, codes.  grid (splits, H, B).
+template <int NT, int CODE, int W>
+__global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : NT < 3 ? 2 : 1) void c8_few_kernel(C8Attn a) {
   const int b = blockIdx.z, h = blockIdx.y, sp = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int x = lane & 15, kb = lane >> 4;
   const int len = min(max(a.length[b], 0), a.cap);
   const int nq = a.q_count ? min(max(a.q_count[b], 0), a.n) : a.n;
   const int rows = a.n * a.rep;
-  const int nb = (len + G - 1) / G, units = 4 * a.splits, un = 4 * sp + w;
+  const int nb = (len + G - 1) / G, units = W * a.splits, un = W * sp + w;
   const int b0 = (int)((long long)un * nb / units), b1 = (int)((long long)(un + 1) * nb / units);
   const int all = a.causal ? max(len - nq + 1, 0) : len;          // tokens that every row sees
   const size_t head = ((size_t)b * a.H + h) * a.nbc;
@@ -259,9 +260,9 @@ __global__ __launch_bounds__(256, NT < 3 ? 2 : 1) void c8_few_kernel(C8Attn a) {
       f = g;
     }
   }
-  // the four waves' sums, a tile of rows at a time
-  __shared__ f4 so[4][16][D / 4 + 1];
-  __shared__ float sm[4][16], sl[4][16];
+  // the waves' sums, a tile of rows at a time
+  __shared__ f4 so[W][16][D / 4 + 1];
+  __shared__ float sm[W][16], sl[W][16];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const float l = row_sum(r, t);
@@ -271,16 +272,16 @@ __global__ __launch_bounds__(256, NT < 3 ? 2 : 1) void c8_few_kernel(C8Attn a) {
     for (int m = 0; m < 8; ++m) so[w][x][4 * m + kb] = r.o[t][m];
     __syncthreads();
 #pragma unroll
-    for (int e = tid; e < 16 * (D / 4); e += 256) {
+    for (int e = tid; e < 16 * (D / 4); e += 64 * W) {
       const int rr = e / (D / 4), c4 = e % (D / 4), row = 16 * t + rr;
       if (row >= rows) continue;
       float M = NONE;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) M = fmaxf(M, sm[k][rr]);
+      for (int k = 0; k < W; ++k) M = fmaxf(M, sm[k][rr]);
       f4 o = f4{0.f, 0.f, 0.f, 0.f};
       float l = 0.0f;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < W; ++k) {
         const float wt = __builtin_amdgcn_exp2f(sm[k][rr] - M);
         o += so[k][rr][c4] * wt;
         l = fmaf(sl[k][rr], wt, l);
@@ -299,12 +300,14 @@ __global__ __launch_bounds__(256, NT < 3 ? 2 : 1) void c8_few_kernel(C8Attn a) {
 // Waves share out the rows: 16 NT a wave, 64 NT a workgroup, which walks the split's blocks together.  Each wave
 // decodes a quarter of a block into LDS, where all four read it as operands, in their order, 16 bytes a lane.  The vector
 // units are the bound, not the matrix cores: a 16 x 16 x 32 product keeps them from issuing for 8 of its 16 cycles, and a
-// block costs a wave some 170 instructions of 4.6 cycles beside 51 products (a score: 1 multiply-add, an exponential of 8.6
-// cycles, half a conversion, half a maximum; the decoding 40).  So: the more rows a wave, the fewer decodings and LDS reads a
-// row - 48 rows are what 256 registers hold, two waves a SIMD (32 rows, three waves: 410 us where this took 352) - the
-// weights of a block are made between the products of the block before, the decoding between those of the scores, and the
-// denominators are products with ones.  196 queries x 28 heads over 98196 tokens, int8: 327 us, 0.84 PFLOP/s (0.94 with the
-// rows that pad the last tile); 6272 over themselves, causal: 321 us, 0.88.
+// block costs a wave some 170 instructions of 4.6 cycles beside 51 products (a score: one multiply-add, an exponential of
+// 8.6 cycles, half a conversion, half a maximum; the decoding: 40).  So: the more rows a wave, the fewer decodings and LDS
+// reads a row - 48 rows are what 256 registers hold, two waves a SIMD (32 rows, three waves: 410 us where 48 took 352) -
+// the weights of a block are made between the products of the block before, the decoding between those of the scores, and
+// the denominators are products with ones.  196 queries x 28 heads over 98196 tokens, int8: 262 us, 1.05 PFLOP/s (1.18 with
+// the rows that pad the last tile); 6272 over themselves, causal: 270 us, 1.04.  On the way there: each wave decoding for
+// itself from memory 902 and 750; the weights in a phase of their own 340 and 350; eight waves to a workgroup, half the
+// decoding each: the same.  32 x 32 x 16 products, which cost the vector units less, with 32 rows a wave: 460 and 355.
 // grid (tiles of rows x splits x B x H), heads fastest: the tiles that see most come first, and what shares a head's
 // codes runs at the same time, where the heads divide the eight dies' turns on the same die.
 template <int NT, int CODE>
@@ -599,23 +602,39 @@ __global__ __launch_bounds__(256) void c8_merge_kernel(C8Attn a) {
 struct C8Plan {
   int nt;                      // row tiles of 16 a wave
   bool few;                    // waves share blocks (all rows fit one wave), else rows
+  int waves;                   // few: a workgroup's
   int tiles, splits;
 };
 
+// Up to 48 rows a head are a wave's, and waves share the blocks.  One round of workgroups is best: each costs some 3 us before
+// its first product and its partials as long behind the last (196000 tokens, 4 heads: 40.8 us with a workgroup a compute
+// unit, 41.5 with two, 44.9 with four; 16 sequences of up to 6001 tokens, 40 rows: 23.6, 28.6, 38.2).
+// Where the heads are three quarters of the compute units or more, for caches of up to 2048 tokens half of them, a workgroup
+// of twelve waves takes a head and there is no merge (64 x 4 heads of 512 tokens 13.2 -> 8.9 us, of 8192 113 -> 91; 1024 heads of
+// 2048 tokens 109 -> 100, but of 384 tokens 19 -> 29; 128 heads of 2048 tokens 16.5 -> 15.1, of 2048 to 4096 23.2 -> 27.8),
+// and so it does for a cache of a block a wave (4 heads of 256 tokens 6.6 -> 5.6; of 1024 tokens 6.9 -> 9.0).  Its sequences
+// may differ in length: then up to four a compute unit, while a wave keeps 16 blocks (64 sequences of 12544 to 25088 tokens:
+// 173 us unsplit, 156 in four; 16 of up to 6272, a block a wave: 19 and 44).
 static C8Plan c8_plan(const C8Geom& g, int n) {
   C8Plan p{};
-  const long long rows = (long long)n * g.rep;
+  const long long rows = (long long)n * g.rep, heads = (long long)g.H * g.B, cu = device_cu_count();
   p.few = rows <= 48;
-  p.nt = !p.few ? 3 : (int)(rows + 15) / 16;
-  p.tiles = p.few ? 1 : (int)((rows + 64 * p.nt - 1) / (64 * p.nt));
-  // two workgroups a compute unit; four where waves share blocks and the sequences' lengths can differ (one layer of 64
-  // sequences of 12544 to 25088 tokens: 170 us with two, 160 with four; one of 196000: 39.0 and 39.8, the merge 4.1 and 5.9);
-  // one where three tiles of rows leave room for one (40 rows, 16 sequences of up to 6001 tokens: 21.6 us, with two 23.9)
-  const long long wgs = (long long)p.tiles * g.H * g.B;
-  const long long want = (!p.few ? 2LL : p.nt == 3 ? 1LL : g.B > 1 ? 4LL : 2LL) * device_cu_count();
-  long long s = (want + wgs - 1) / wgs;
-  const long long most = p.few ? (g.nbc + 3) / 4 : (g.nbc + 7) / 8;
-  p.splits = (int)std::max(1LL, std::min({s, most, 256LL}));
+  if (!p.few) {
+    p.nt = 3;
+    p.tiles = (int)((rows + 64 * p.nt - 1) / (64 * p.nt));
+    const long long wgs = p.tiles * heads;                     // two workgroups a compute unit
+    p.splits = (int)std::max(1LL, std::min({(2 * cu + wgs - 1) / wgs, (g.nbc + 7LL) / 8, 256LL}));
+    return p;
+  }
+  p.nt = (int)(rows + 15) / 16;
+  p.tiles = 1;
+  const bool filled = 4 * heads >= 3 * cu || (2 * heads >= cu && g.nbc <= 64);
+  const bool wide = p.nt == 1 && (filled ? heads < 4 * cu || g.nbc >= 40 : g.nbc <= 12);
+  p.waves = wide ? 12 : 4;
+  const long long fill = (cu + heads - 1) / heads;
+  long long s = wide ? 1 : fill;
+  if (filled) s = std::max(s, std::min(g.B > 1 ? std::max(fill, 4 * cu / heads) : fill, (long long)g.nbc / (16 * p.waves)));
+  p.splits = (int)std::max(1LL, std::min({s, (g.nbc + 3LL) / 4, 256LL}));
   return p;
 }
 
@@ -671,9 +690,10 @@ hipError_t launch_c8_attn(const C8Geom& g, int layer, int n, int causal, float s
   auto by_code = [&](auto code) {
     constexpr int CODE = decltype(code)::value;
     const dim3 few(p.splits, g.H, g.B);
-    if (p.few && p.nt == 1) hipLaunchKernelGGL((c8_few_kernel<1, CODE>), few, blk, 0, st, a);
-    else if (p.few && p.nt == 2) hipLaunchKernelGGL((c8_few_kernel<2, CODE>), few, blk, 0, st, a);
-    else if (p.few) hipLaunchKernelGGL((c8_few_kernel<3, CODE>), few, blk, 0, st, a);
+    if (p.few && p.waves == 12) hipLaunchKernelGGL((c8_few_kernel<1, CODE, 12>), few, dim3(768), 0, st, a);
+    else if (p.few && p.nt == 1) hipLaunchKernelGGL((c8_few_kernel<1, CODE, 4>), few, blk, 0, st, a);
+    else if (p.few && p.nt == 2) hipLaunchKernelGGL((c8_few_kernel<2, CODE, 4>), few, blk, 0, st, a);
+    else if (p.few) hipLaunchKernelGGL((c8_few_kernel<3, CODE, 4>), few, blk, 0, st, a);
     else hipLaunchKernelGGL((c8_many_kernel<3, CODE>), dim3(p.tiles * p.splits * g.H * g.B), blk, 0, st, a, p.tiles);
   };
   if (g.code == 0) by_code(std::integral_constant<int, 0>{});

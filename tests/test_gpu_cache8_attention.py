@@ -142,6 +142,31 @@ def test_long(B, H, rep, n, T, code, dtype):
 
 
 @pytest.mark.parametrize("code", [0, 1])
+def test_many_heads(code):
+    """As many heads as compute units, short and long (a workgroup a head, and several): sampled sequences against a cache of
+    their own, which the other ways of sharing the work go through."""
+    for B, H, rep, cap in ((128, 2, 7, 96), (96, 2, 4, 12320), (300, 4, 1, 64), (1100, 1, 2, 320)):
+        print(f"[case] many heads B={B} H={H} cap={cap}", flush=True)
+        g = torch.Generator(device=DEV)
+        g.manual_seed(40 + B)
+        lens = [(cap - 7 * b) % (cap + 1) for b in range(B)]
+        K, V = (torch.randn((B, H, cap, 128), generator=g, device=DEV, dtype=torch.float16) for _ in range(2))
+        p = vk.make_cache8(1, B, H, H * rep, cap, code)
+        buf = vk.alloc_bytes(vk.cache8_bytes(p), DEV)
+        buf.fill_(0xFF)
+        vk.cache8_write(p, 0, buf, K, V, i32([0] * B), i32(lens))
+        q = queries(B, H * rep, 1, F16, 41)
+        out = attend(p, 0, buf, q, lens)
+        for b in (0, 1, B // 2, B - 1):
+            one = vk.make_cache8(1, 1, H, H * rep, cap, code)
+            small = vk.alloc_bytes(vk.cache8_bytes(one), DEV)
+            small.fill_(0xFF)
+            vk.cache8_write(one, 0, small, K[b:b + 1], V[b:b + 1], i32([0]), i32([lens[b]]))
+            check(one, 0, small, q[b:b + 1], out[b:b + 1], [lens[b]])
+        del K, V, buf
+
+
+@pytest.mark.parametrize("code", [0, 1])
 def test_wild_magnitudes_and_queries(code):
     """Blocks whose values differ by 2^24, scores that take the whole softmax, queries from 1e-6 to 1e4."""
     for dtype, size in ((F16, 1.0), (F16, 50.0), (BF16, 1e4), (BF16, 1e-6), (BF16, 3.0)):
