@@ -321,8 +321,6 @@ __global__ __launch_bounds__(256, 2) void c8_many_kernel(C8Attn a, int tiles) {
   const int len = min(max(a.length[b], 0), a.cap);
   const int nq = a.q_count ? min(max(a.q_count[b], 0), a.n) : a.n;
   const int rows = a.n * a.rep, tile0 = tile * 64 * NT, row0 = tile0 + w * 16 * NT;
-  Rows<NT> r;
-  load_rows<NT>(r, a, b, h, row0, rows, len, nq, lane);
   // tokens that the first row from `row` on sees, and those that the last of `n` rows does
   auto least = [&](int row) { return row / a.rep >= nq ? 0 : a.causal ? max(len - nq + row / a.rep + 1, 0) : len; };
   auto most = [&](int row, int n) {
@@ -356,6 +354,17 @@ __global__ __launch_bounds__(256, 2) void c8_many_kernel(C8Attn a, int tiles) {
   auto put_v = [&](int i, int e) { ops[i & 1][8 + 2 * w + e][lane] = decode8<CODE>(gv[2 * e], gv[2 * e + 1]); };
   // LDS alone is handed over: what is still on its way from memory goes on
   auto hand_over = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+  // the first two blocks' codes, on their way while the queries are laid out
+  u32x4 gk0{};
+  float km = 1.0f, vm = 1.0f;
+  if (b0 < b1) {
+    ask_k(b0);
+    gk0 = gk; km = gkm; vm = gvm;
+    ask_v(b0);
+    ask_k(b0 + 1);
+  }
+  Rows<NT> r;
+  load_rows<NT>(r, a, b, h, row0, rows, len, nq, lane);
   f4 s[NT][2];
   Op p[NT], n0, n1;
   float al[NT];
@@ -435,15 +444,12 @@ __global__ __launch_bounds__(256, 2) void c8_many_kernel(C8Attn a, int tiles) {
     for (int t = 0; t < NT; ++t) { ck[t] = r.cq[t] * km; off[t] = lv + UP - r.m[t]; }
   };
   if (b0 < b1) {
-    ask_k(b0);
-    ask_v(b0);
     clear_dead(b0);
-    put_k(b0, 0); put_k(b0, 1);
     put_v(b0, 0); put_v(b0, 1);
-    float km = gkm, vm = gvm;
-    ask_k(b0 + 1);
     put_k(b0 + 1, 0); put_k(b0 + 1, 1);
     float kn = gkm, vn = gvm;              // of the next block
+    gk = gk0;
+    put_k(b0, 0); put_k(b0, 1);
     ask_k(b0 + 2);
     ask_v(b0 + 1);
     hand_over();
@@ -620,10 +626,21 @@ static C8Plan c8_plan(const C8Geom& g, int n) {
   const long long rows = (long long)n * g.rep, heads = (long long)g.H * g.B, cu = device_cu_count();
   p.few = rows <= 48;
   if (!p.few) {
-    p.nt = 3;
+    p.nt = rows <= 64 ? 1 : rows <= 128 ? 2 : 3;
     p.tiles = (int)((rows + 64 * p.nt - 1) / (64 * p.nt));
-    const long long wgs = p.tiles * heads;                     // two workgroups a compute unit
-    p.splits = (int)std::max(1LL, std::min({(2 * cu + wgs - 1) / wgs, (g.nbc + 7LL) / 8, 256LL}));
+    // Splits, up to two workgroups a compute unit, by what they cost: a block takes a workgroup 0.9 to 1.1 us where it has
+    // the unit for itself, 1.0 to 1.65 beside another; a row's partials are 528 bytes written and read, at 5 TB/s, the
+    // merge's launch 4 us.  (112 rows of 256 heads over 1024 tokens: 31.0 us unsplit, 35.4 in two; 56 rows over 4096: 109 and 78;
+    // 1372 rows of 32 heads over 512: 23 and 36.)
+    const long long wgs = p.tiles * heads;
+    const int most = (int)std::min({(2 * cu + wgs - 1) / wgs, (g.nbc + 7LL) / 8, 256LL});
+    const float alone = 0.8f + 0.1f * p.nt, beside = p.nt == 1 ? 1.0f : p.nt == 2 ? 1.25f : 1.65f;
+    float least = 0.0f;
+    for (int k = 1; k <= std::max(most, 1); ++k) {
+      const float us = (float)g.nbc / k * (wgs * k <= cu ? alone : beside) +
+                       (k > 1 ? 4.0f + (float)heads * (float)rows * k * (2 * 528 / 5e6f) : 0.0f);
+      if (k == 1 || us < least) { least = us; p.splits = k; }
+    }
     return p;
   }
   p.nt = (int)(rows + 15) / 16;
@@ -650,7 +667,7 @@ size_t c8_attn_ws_bytes(const C8Geom& g, int n) {
   size_t most = 0;
   for (long long q = 1; q <= n;) {
     const C8Plan p = c8_plan(g, (int)q);
-    if (!p.few && p.splits == 1) break;
+    if (p.nt == 3 && !p.few && p.splits == 1) break;
     const long long rows = p.few ? 16LL * p.nt : 64LL * p.nt * p.tiles;          // the last of this plan
     const long long last = std::max(q, std::min<long long>(n, rows / g.rep));
     most = std::max(most, c8_parts(g, last * g.rep, p.splits));
@@ -689,12 +706,14 @@ hipError_t launch_c8_attn(const C8Geom& g, int layer, int n, int causal, float s
   const dim3 blk(256);
   auto by_code = [&](auto code) {
     constexpr int CODE = decltype(code)::value;
-    const dim3 few(p.splits, g.H, g.B);
+    const dim3 few(p.splits, g.H, g.B), many(p.tiles * p.splits * g.H * g.B);
     if (p.few && p.waves == 12) hipLaunchKernelGGL((c8_few_kernel<1, CODE, 12>), few, dim3(768), 0, st, a);
     else if (p.few && p.nt == 1) hipLaunchKernelGGL((c8_few_kernel<1, CODE, 4>), few, blk, 0, st, a);
     else if (p.few && p.nt == 2) hipLaunchKernelGGL((c8_few_kernel<2, CODE, 4>), few, blk, 0, st, a);
     else if (p.few) hipLaunchKernelGGL((c8_few_kernel<3, CODE, 4>), few, blk, 0, st, a);
-    else hipLaunchKernelGGL((c8_many_kernel<3, CODE>), dim3(p.tiles * p.splits * g.H * g.B), blk, 0, st, a, p.tiles);
+    else if (p.nt == 1) hipLaunchKernelGGL((c8_many_kernel<1, CODE>), many, blk, 0, st, a, p.tiles);
+    else if (p.nt == 2) hipLaunchKernelGGL((c8_many_kernel<2, CODE>), many, blk, 0, st, a, p.tiles);
+    else hipLaunchKernelGGL((c8_many_kernel<3, CODE>), many, blk, 0, st, a, p.tiles);
   };
   if (g.code == 0) by_code(std::integral_constant<int, 0>{});
   else by_code(std::integral_constant<int, 1>{});

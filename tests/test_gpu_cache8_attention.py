@@ -121,6 +121,8 @@ def test_single_tokens(B, H, rep, cap, lens, code, dtype):
     (3, 2, 8, 2, 96, [0, 1, 70], None), (2, 1, 7, 3, 512, [2, 500], [3, 1]), (2, 2, 8, 5, 256, [3, 251], None),
     (4, 1, 1, 17, 64, [17, 5, 64, 33], [17, 17, 0, 40]), (2, 2, 7, 37, 320, [300, 37], None),
     (1, 1, 4, 130, 160, [130], None), (2, 1, 7, 100, 640, [640, 20], [99, 100]), (1, 2, 1, 300, 320, [310], None),
+    (3, 2, 7, 8, 1024, [1000, 8, 3], [8, 5, 8]), (2, 1, 7, 16, 2048, [2048, 33], None), (2, 1, 8, 24, 512, [480, 25], None),
+    (2, 1, 64, 1, 320, [320, 1], None), (1, 1, 65, 2, 96, [70], None),
 ])
 def test_several_queries(B, H, rep, n, cap, lens, counts, causal, code, dtype):
     print(f"[case] several B={B} H={H} rep={rep} n={n} cap={cap} code={code}", flush=True)
