@@ -385,7 +385,8 @@ size_t vidkv_cache8_workspace_bytes(const vidkv_cache8 *p, int32_t n_query);
  * cache held before are given up.  A block that begins before start[b] keeps its
  * live tokens: where the new ones raise its magnitude from A to A', their codes c
  * become the code of value(c) (in the code's units) * A / A'; else they are not
- * touched.  Codes behind the last new token are left as they were.
+ * touched (those tokens have to have been written, or the buffer cleared).  Codes
+ * behind the last new token are left as they were.
  *   K, V      in : [B, Hkv, n_tokens, 128], fp16 or bf16, both the same dtype;
  *                  rows from count[b] on are not read
  *   start_dev in : [B] int32; a negative start writes nothing for the sequence,
@@ -415,7 +416,9 @@ vidkv_status vidkv_cache8_read(const vidkv_cache8 *p, int32_t layer, int32_t n_t
  * The queries are the last ones of the sequence: query i of q_count[b] stands at
  * token length[b] - q_count[b] + i and, with causal = 1, sees the tokens up to
  * itself; with causal = 0 all.  A query that sees no token, and the rows from
- * q_count[b] on, get zeros.
+ * q_count[b] on, get zeros.  Scores scale * q.k are held in fp32: a weight's
+ * relative error is some 2^-24 of the largest of them (which is why they are to
+ * stay below 2^24; beyond, weights are unspecified).
  *   q         in : [B, Hq, n_query, 128], fp16 or bf16
  *   out      out : likewise, of q's dtype (fp32 accumulation)
  *   length_dev in: [B] int32, taken as 0..capacity

@@ -51,7 +51,9 @@ __device__ __forceinline__ uint32_t lane_xor8(uint32_t v) {
 // sides of eight pairs where the keys are turned); V: wave = lane group kb of the record, lane = two channels of its eight
 // tokens, so that its codes are whole 8-byte pieces of the record, and two lanes' four pieces two whole 16-byte ones.
 // What a workgroup waits for - rows, positions, a begun block's magnitudes and codes - is asked for as soon as its block
-// is known.  grid (blocks a sequence can reach, H, B).
+// is known.  8 x 4 heads x 12544 tokens in fp16: 67 us for 308 MB, 4.6 TB/s; the vector units are the second bound, 9
+// instructions an element of which the exact quotient is 4 (with a branch a row, values in 8-byte stores at every second place
+// and maxima in float32: 84 us).  One token of 64 sequences, turned: 5.9 us.  grid (blocks a sequence can reach, H, B).
 template <class T, int CODE, bool ROT>
 __global__ __launch_bounds__(256) void c8_write_kernel(C8Write a) {
   // (all arguments in one round trip; left to itself the compiler asks for each where it is used)
@@ -262,7 +264,8 @@ struct C8Read {
   int H, nbc, cap;
 };
 
-// One workgroup per block that the asked-for tokens lie in, threads as above.
+// One workgroup per block that the asked-for tokens lie in, threads as above.  8 x 4 heads x 12544 tokens as fp16: 56 us for
+// 308 MB, 5.5 TB/s.
 template <class T, int CODE>
 __global__ __launch_bounds__(256) void c8_read_kernel(C8Read a) {
   const int b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;

@@ -180,6 +180,33 @@ def test_wild_magnitudes_and_queries(code):
             check(p, 0, buf, q, attend(p, 0, buf, q, [640, 333]), [640, 333])
 
 
+def test_scores_at_the_ends_of_float():
+    """Scores that vanish (equal weights) beside masked tokens, keys of the least magnitude.  Weights are exact here but for
+    fp16's half step and log2's and exp2's last bits.  (Scores of 2^24 and more are not the interface's: S in the bound above
+    is then 2^24 u = 1 and more in a weight's exponent.)"""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(50)
+    for key, query, scale in ((2.0 ** -41, 1e-35, 1e-30), (1.0, 1e-36, SCALE), (2.0 ** -20, 1e-30, SCALE)):
+        p = vk.make_cache8(1, 1, 1, 3, 96, 0, softmax_scale=scale)
+        buf = vk.alloc_bytes(vk.cache8_bytes(p), DEV)
+        K = torch.zeros((1, 1, 96, 128), device=DEV)
+        K[..., 0] = key * (1 + torch.arange(96, device=DEV) / 256)             # ascending: the last seen token has the largest score
+        V = torch.randn((1, 1, 96, 128), generator=g, device=DEV)
+        vk.cache8_write(p, 0, buf, K.bfloat16(), V.bfloat16(), i32([0]))
+        kc, vc, km, vm = O.unpack(buf.cpu().numpy(), 1, 1, 1, 96)
+        Kd, Vd = O.values(kc[0, 0, 0], km[0, 0, 0], 0), O.values(vc[0, 0, 0], vm[0, 0, 0], 0)
+        for n, T in ((1, 70), (40, 70), (1, 96)):
+            q = torch.full((1, 3, n, 128), query, dtype=torch.float32, device=DEV).bfloat16()
+            out = attend(p, 0, buf, q, [T]).double().cpu().numpy()
+            for i in range(n):
+                t = T - n + i + 1
+                x = (Kd[:t, 0] * float(query)).astype(np.float64) * scale
+                w = np.exp(np.clip(x - x.max(), -1e4, 0))
+                ref = (w / w.sum()) @ Vd[:t]
+                tol = (np.abs(Vd[:t]).max() * 2.0 ** -10 + 2.0 ** -8 * np.abs(ref))
+                assert (np.abs(out[0, :, i] - ref) <= tol).all(), (key, query, n, i)
+
+
 def test_rising_scores():
     """Every block's scores above all before by more than the maximum's slack: the running sums are rescaled each time."""
     p = vk.make_cache8(1, 1, 1, 2, 1024, 0)
