@@ -88,10 +88,6 @@ struct TF16 {
   static __device__ __forceinline__ Run load(const void* p) { return *static_cast<const h8*>(p); }
   static __device__ __forceinline__ f8v widen(Run v) { return __builtin_convertvector(v, f8v); }
   static __device__ __forceinline__ void store(void* p, f8v v) { store8(p, v); }
-  static __device__ __forceinline__ f8v load8(const void* p) {
-    const h8 v = *static_cast<const h8*>(p);
-    return __builtin_convertvector(v, f8v);
-  }
   static __device__ __forceinline__ void store8(void* p, f8v v) { *static_cast<h8*>(p) = __builtin_convertvector(v, h8); }
   static __device__ __forceinline__ f2 widen2(uint32_t u) {
     const h2 v = bits_h2(u);
@@ -111,7 +107,6 @@ struct TBF16 {
   typedef u32x4 Run;
   static __device__ __forceinline__ Run load(const void* p) { return *static_cast<const u32x4*>(p); }
   static __device__ __forceinline__ void store(void* p, f8v v) { store8(p, v); }
-  static __device__ __forceinline__ f8v load8(const void* p) { return widen(load(p)); }
   static __device__ __forceinline__ f8v widen(Run u) {
     f8v r;
 #pragma unroll
@@ -139,10 +134,6 @@ struct TF32 {
   static __device__ __forceinline__ Run load(const void* p) { return *static_cast<const f4*>(p); }
   static __device__ __forceinline__ f4 widen(Run v) { return v; }
   static __device__ __forceinline__ void store(void* p, f4 v) { *static_cast<f4*>(p) = v; }
-  static __device__ __forceinline__ f8v load8(const void* p) {
-    const f4 a = static_cast<const f4*>(p)[0], b = static_cast<const f4*>(p)[1];
-    return f8v{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-  }
   static __device__ __forceinline__ void store8(void* p, f8v v) {
     static_cast<f4*>(p)[0] = f4{v[0], v[1], v[2], v[3]};
     static_cast<f4*>(p)[1] = f4{v[4], v[5], v[6], v[7]};
@@ -171,6 +162,34 @@ __device__ __forceinline__ void turn_cos_sin(int pos, uint64_t turn, float* c, f
   const float a = (q & 1) ? si : co, b = (q & 1) ? co : si;      // |cos|, |sin| up to sign
   *c = (q == 1 || q == 2) ? -a : a;
   *s = (q & 2) ? -b : b;
+}
+
+// A pair turned; in one order of roundings, so that every kernel that turns it leaves the same bits.
+__device__ __forceinline__ void turn_pair(float& a, float& b, float c, float s) {
+  const float x1 = a, x2 = b;
+  a = fmaf(x1, c, -(x2 * s));
+  b = fmaf(x2, c, x1 * s);
+}
+
+// Two runs of N elements, the two sides of N pairs; or, adjacent, N / 2 pairs each.
+template <int N, class V>
+__device__ __forceinline__ void turn_runs(V& x, V& y, bool adjacent, const float* co, const float* si) {
+  if (adjacent) {
+#pragma unroll
+    for (int e = 0; e < N / 2; ++e) {
+      float a = x[2 * e], b = x[2 * e + 1], c = y[2 * e], d = y[2 * e + 1];
+      turn_pair(a, b, co[e], si[e]);
+      turn_pair(c, d, co[N / 2 + e], si[N / 2 + e]);
+      x[2 * e] = a; x[2 * e + 1] = b; y[2 * e] = c; y[2 * e + 1] = d;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      float a = x[e], b = y[e];
+      turn_pair(a, b, co[e], si[e]);
+      x[e] = a; y[e] = b;
+    }
+  }
 }
 
 // ---- codes ----------------------------------------------------------------------------------

@@ -125,23 +125,7 @@ __global__ __launch_bounds__(256) void c8_write_kernel(C8Write a) {
         const int ax = a.rot.axis[8 * u + e];
         turn_cos_sin(ax & 2 ? (ax & 1 ? pos[3] : pos[2]) : (ax & 1 ? pos[1] : pos[0]), a.rot.turn[8 * u + e], &co[e], &si[e]);
       }
-      if (a.rot.adjacent) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float x1 = x[2 * e], x2 = x[2 * e + 1], y1 = y[2 * e], y2 = y[2 * e + 1];
-          x[2 * e] = x1 * co[e] - x2 * si[e];
-          x[2 * e + 1] = x2 * co[e] + x1 * si[e];
-          y[2 * e] = y1 * co[4 + e] - y2 * si[4 + e];
-          y[2 * e + 1] = y2 * co[4 + e] + y1 * si[4 + e];
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float x1 = x[e], x2 = y[e];
-          x[e] = x1 * co[e] - x2 * si[e];
-          y[e] = x2 * co[e] + x1 * si[e];
-        }
-      }
+      turn_runs<8>(x, y, a.rot.adjacent, co, si);
     }
   }
 

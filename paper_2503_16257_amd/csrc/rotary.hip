@@ -64,25 +64,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
       r0 = T::load(at(h + 1, a.q, a.k) + c0 * T::BYTES);
       r1 = T::load(at(h + 1, a.q, a.k) + c1 * T::BYTES);
     }
-    if (turns) {
-      if (a.rot.adjacent) {
-#pragma unroll
-        for (int e = 0; e < E / 2; ++e) {
-          const float x1 = x[2 * e], x2 = x[2 * e + 1], y1 = y[2 * e], y2 = y[2 * e + 1];
-          x[2 * e] = x1 * co[e] - x2 * si[e];
-          x[2 * e + 1] = x2 * co[e] + x1 * si[e];
-          y[2 * e] = y1 * co[E / 2 + e] - y2 * si[E / 2 + e];
-          y[2 * e + 1] = y2 * co[E / 2 + e] + y1 * si[E / 2 + e];
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float x1 = x[e], x2 = y[e];
-          x[e] = x1 * co[e] - x2 * si[e];
-          y[e] = x2 * co[e] + x1 * si[e];
-        }
-      }
-    }
+    if (turns) turn_runs<E>(x, y, a.rot.adjacent, co, si);
     char* out = const_cast<char*>(at(h, a.qo, a.ko));
     T::store(out + c0 * T::BYTES, x);
     T::store(out + c1 * T::BYTES, y);
