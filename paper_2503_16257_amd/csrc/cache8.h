@@ -81,7 +81,7 @@ inline Rot make_rot(const vidkv_rotary* r, const int32_t* pos, long long rows) {
 // ---- element types --------------------------------------------------------------------------
 typedef float f8v __attribute__((ext_vector_type(8)));
 
-// (Run: 16 bytes as they lie in memory)
+// (Run: 16 bytes as they lie in memory, Run2: two elements)
 struct TF16 {
   static constexpr int BYTES = 2;
   typedef h8 Run;
@@ -89,6 +89,8 @@ struct TF16 {
   static __device__ __forceinline__ f8v widen(Run v) { return __builtin_convertvector(v, f8v); }
   static __device__ __forceinline__ void store(void* p, f8v v) { store8(p, v); }
   static __device__ __forceinline__ void store8(void* p, f8v v) { *static_cast<h8*>(p) = __builtin_convertvector(v, h8); }
+  typedef uint32_t Run2;
+  static __device__ __forceinline__ Run2 load2(const void* p) { return *static_cast<const uint32_t*>(p); }
   static __device__ __forceinline__ f2 widen2(uint32_t u) {
     const h2 v = bits_h2(u);
     return f2{(float)v[0], (float)v[1]};
@@ -117,6 +119,8 @@ struct TBF16 {
     return r;
   }
   static __device__ __forceinline__ void store8(void* p, f8v v) { *static_cast<b8*>(p) = __builtin_convertvector(v, b8); }
+  typedef uint32_t Run2;
+  static __device__ __forceinline__ Run2 load2(const void* p) { return *static_cast<const uint32_t*>(p); }
   static __device__ __forceinline__ f2 widen2(uint32_t u) {
     return f2{__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u)};
   }
@@ -138,6 +142,9 @@ struct TF32 {
     static_cast<f4*>(p)[0] = f4{v[0], v[1], v[2], v[3]};
     static_cast<f4*>(p)[1] = f4{v[4], v[5], v[6], v[7]};
   }
+  typedef f2 Run2;
+  static __device__ __forceinline__ Run2 load2(const void* p) { return *static_cast<const f2*>(p); }
+  static __device__ __forceinline__ f2 widen2(Run2 v) { return v; }
   static __device__ __forceinline__ void store2(void* p, float a, float b) { *static_cast<f2*>(p) = f2{a, b}; }
 };
 

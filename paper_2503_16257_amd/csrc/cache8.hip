@@ -42,6 +42,8 @@ __device__ __forceinline__ us2 wave_max(us2 v) {
 // A block's magnitude as it is stored: never zero, and bounded so that no product with it leaves float's range.
 __device__ __forceinline__ float bounded(float a) { return fminf(fmaxf(a, C8_LEAST), C8_MOST); }
 
+constexpr int FEW = 8;                     // new tokens of a block whose sines are shared out
+
 // The lane eight further on in its row of sixteen.
 __device__ __forceinline__ uint32_t lane_xor8(uint32_t v) {
   return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xf, 0xf, true);      // row_ror:8
@@ -53,7 +55,7 @@ __device__ __forceinline__ uint32_t lane_xor8(uint32_t v) {
 // What a workgroup waits for - rows, positions, a begun block's magnitudes and codes - is asked for as soon as its block
 // is known.  8 x 4 heads x 12544 tokens in fp16: 67 us for 308 MB, 4.6 TB/s; the vector units are the second bound, 9
 // instructions an element of which the exact quotient is 4 (with a branch a row, values in 8-byte stores at every second place
-// and maxima in float32: 84 us).  One token of 64 sequences, turned: 5.9 us.  grid (blocks a sequence can reach, H, B).
+// and maxima in float32: 84 us).  One token of 64 sequences, turned: 5.3 us.  grid (blocks a sequence can reach, H, B).
 template <class T, int CODE, bool ROT>
 __global__ __launch_bounds__(256) void c8_write_kernel(C8Write a) {
   // (all arguments in one round trip; left to itself the compiler asks for each where it is used)
@@ -109,25 +111,46 @@ __global__ __launch_bounds__(256) void c8_write_kernel(C8Write a) {
     k0 = *pk0; k1 = *pk1;
   }
   if (!whole) vold = *pv;
-  int pos[4] = {0, 0, 0, 0};
-  if constexpr (ROT) {
-    const long long row = (long long)b * a.n + (knew ? kt - start : 0);
+  auto sines = [&](int token, int pair, float* co, float* si) {           // of new token `token` of the sequence
+    const long long row = (long long)b * a.n + token;
+    int pos[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) pos[i] = a.rot.pos[min(i, a.n_axes - 1) * a.rot.rows + row];
-  }
-  ko = bounded(ko); vo = bounded(vo);
-  f8v x = T::widen(rx), y = T::widen(ry);
+    const int ax = a.rot.axis[pair];
+    turn_cos_sin(ax & 2 ? (ax & 1 ? pos[3] : pos[2]) : (ax & 1 ? pos[1] : pos[0]), a.rot.turn[pair], co, si);
+  };
+  f8v x, y;
   if constexpr (ROT) {
+    // A token's sines are eight threads' work; those of few tokens are shared out to all (one token of 64 sequences: 5.7 -> 5.3 us)
+    __shared__ f2 table[FEW][D / 2];
+    const int pairs = a.rot.rot_dim / 2, fresh = hi - lo;
+    float co[8], si[8];
+    if (fresh <= FEW) {
+      for (int i = tid; i < fresh * pairs; i += 256) {
+        const int t = i / pairs, e = i - t * pairs;
+        float c, s;
+        sines(lo - start + t, e, &c, &s);
+        table[t][e] = f2{c, s};
+      }
+      __syncthreads();
+    }
+    x = T::widen(rx); y = T::widen(ry);
     if (turns && knew) {
-      float co[8], si[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const int ax = a.rot.axis[8 * u + e];
-        turn_cos_sin(ax & 2 ? (ax & 1 ? pos[3] : pos[2]) : (ax & 1 ? pos[1] : pos[0]), a.rot.turn[8 * u + e], &co[e], &si[e]);
+        if (fresh <= FEW) {
+          const f2 v = table[kt - lo][8 * u + e];
+          co[e] = v[0]; si[e] = v[1];
+        } else {
+          sines(kt - start, 8 * u + e, &co[e], &si[e]);
+        }
       }
       turn_runs<8>(x, y, a.rot.adjacent, co, si);
     }
+  } else {
+    x = T::widen(rx); y = T::widen(ry);
   }
+  ko = bounded(ko); vo = bounded(vo);
 
   // magnitudes of 16-bit numbers compare as integers do, two at a time
   us2 vm{0, 0}, km{0, 0};

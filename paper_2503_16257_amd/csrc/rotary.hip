@@ -3,7 +3,7 @@
 // forward and inverse (the backward pass).  2 x the element's bytes of traffic an element and about four
 // operations: bound by HBM, for single tokens by the launch.  cos and sin belong to a (token, pair), not to a head: a thread
 // makes those of its pairs once and turns them in one or two heads.  6272 tokens of 32 heads x 128 in bf16: 18 us for 103 MB;
-// 3 x 4097 of 32 x 80 in float32, inverse: 46 us for 252 MB, 5.5 TB/s; one token 3.7 us.
+// 3 x 4097 of 32 x 80 in float32, inverse: 46 us for 252 MB, 5.5 TB/s; one token 2.7 us.
 #include "cache8.h"
 
 namespace vidkv {
@@ -19,17 +19,33 @@ struct RotaryArgs {
   Rot rot;
 };
 
-// A unit is two runs of 16 bytes of a token's head: the two sides of as many pairs as a run has elements, or 32 bytes
-// behind rot_dim.  Thread = one unit of one token in `per` heads.  What a thread waits for is asked for at once: the pairs'
+// A unit is two runs of E elements of a token's head: the two sides of E pairs, or 2 E channels behind rot_dim.  Runs are 16
+// bytes, or, where the tokens are few, two elements: what a thread then waits for is its chain of sines, not its bytes.
+// Thread = one unit of one token in `per` heads.  What a thread waits for is asked for at once: the pairs'
 // axes and turns, the positions of every axis, the first head's channels.
 // grid (ceil(rows / tokens a workgroup), ceil(heads / per)).
+template <class T, int E>
+struct RotaryRun {                         // 16 bytes
+  typedef typename T::Run Raw;
+  static __device__ __forceinline__ Raw load(const char* p) { return T::load(p); }
+  static __device__ __forceinline__ auto widen(Raw r) { return T::widen(r); }
+  template <class V> static __device__ __forceinline__ void store(char* p, V v) { T::store(p, v); }
+};
 template <class T>
+struct RotaryRun<T, 2> {
+  typedef typename T::Run2 Raw;
+  static __device__ __forceinline__ Raw load(const char* p) { return T::load2(p); }
+  static __device__ __forceinline__ f2 widen(Raw r) { return T::widen2(r); }
+  static __device__ __forceinline__ void store(char* p, f2 v) { T::store2(p, v[0], v[1]); }
+};
+
+template <class T, int E>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
   // (all arguments in one round trip; left to itself the compiler asks for each where it is used)
   asm volatile("" :: "s"(a.q.data), "s"(a.q.sb), "s"(a.q.sh), "s"(a.q.st), "s"(a.k.data), "s"(a.k.sb), "s"(a.k.sh), "s"(a.k.st),
                "s"(a.qo.data), "s"(a.ko.data), "s"(a.Hq), "s"(a.Hk), "s"(a.n), "s"(a.rows), "s"(a.per), "s"(a.rot.pos),
                "s"(a.rot.head_dim), "s"(a.rot.rot_dim), "s"(a.rot.adjacent), "s"(a.n_axes));
-  constexpr int E = 16 / T::BYTES;         // elements a run
+  typedef RotaryRun<T, E> R;
   typedef float fe __attribute__((ext_vector_type(E)));
   const int U = a.rot.head_dim / (2 * E), tpw = 256 / U;
   const int tok = threadIdx.x / U, u = threadIdx.x - tok * U;
@@ -45,7 +61,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
     const int hh = h < a.Hq ? h : h - a.Hq;
     return v.data + b * v.sb + hh * v.sh + t * v.st;
   };
-  typename T::Run r0 = T::load(at(h0, a.q, a.k) + c0 * T::BYTES), r1 = T::load(at(h0, a.q, a.k) + c1 * T::BYTES);
+  typename R::Raw r0 = R::load(at(h0, a.q, a.k) + c0 * T::BYTES), r1 = R::load(at(h0, a.q, a.k) + c1 * T::BYTES);
   float co[E], si[E];
   if (turns) {
     int pos[4];
@@ -59,15 +75,15 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
     }
   }
   for (int h = h0; h < h1; ++h) {
-    fe x = T::widen(r0), y = T::widen(r1);
+    fe x = R::widen(r0), y = R::widen(r1);
     if (h + 1 < h1) {                      // the next head's, in flight meanwhile
-      r0 = T::load(at(h + 1, a.q, a.k) + c0 * T::BYTES);
-      r1 = T::load(at(h + 1, a.q, a.k) + c1 * T::BYTES);
+      r0 = R::load(at(h + 1, a.q, a.k) + c0 * T::BYTES);
+      r1 = R::load(at(h + 1, a.q, a.k) + c1 * T::BYTES);
     }
     if (turns) turn_runs<E>(x, y, a.rot.adjacent, co, si);
     char* out = const_cast<char*>(at(h, a.qo, a.ko));
-    T::store(out + c0 * T::BYTES, x);
-    T::store(out + c1 * T::BYTES, y);
+    R::store(out + c0 * T::BYTES, x);
+    R::store(out + c1 * T::BYTES, y);
   }
 }
 
@@ -80,16 +96,25 @@ hipError_t launch_rotary(const vidkv_rotary* r, int inverse, int B, int n, const
   a.sign = inverse ? -1.0f : 1.0f;
   a.n_axes = r->n_axes;
   a.rot = make_rot(r, pos, a.rows);
-  const int heads = a.Hq + a.Hk, tpw = 256 / (r->head_dim * dtype_bytes(dtype) / 32);
+  const int heads = a.Hq + a.Hk;
+  // (32 heads of one token, the kernel: 2.7 us with runs of two elements, 3.7 with 16 bytes; calls among others 4.9 and 5.5, of
+  // 64 tokens 4.8 and 4.8, of 400 4.9 and 4.8)
+  const bool short_runs = (long long)a.rows * heads <= 2048;
+  const int run = short_runs ? 2 : 16 / dtype_bytes(dtype), tpw = 256 / (r->head_dim / (2 * run));
   const int tiles = (a.rows + tpw - 1) / tpw;
   // two heads a thread where that leaves a workgroup a compute unit or so (32 heads x 6272 tokens in bf16, one, two, four and
   // eight heads: 29.1, 22.8, 22.3, 23.7 us; x 1000: 6.4, 5.6, 5.7, 7.0; x 64 of one token: 4.5, 4.7, 4.7, 6.1); a thread of
   // float32 makes half as many sines (3 x 4097 tokens of 32 heads: 46.5, 47.9, 49.4, 50.9)
-  a.per = dtype != VIDKV_F32 && (long long)tiles * heads >= 256 ? 2 : 1;
+  a.per = dtype != VIDKV_F32 && !short_runs && (long long)tiles * heads >= 256 ? 2 : 1;
   const dim3 grid(tiles, (heads + a.per - 1) / a.per);
-  if (dtype == VIDKV_F16) hipLaunchKernelGGL(rotary_kernel<TF16>, grid, dim3(256), 0, st, a);
-  else if (dtype == VIDKV_BF16) hipLaunchKernelGGL(rotary_kernel<TBF16>, grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(rotary_kernel<TF32>, grid, dim3(256), 0, st, a);
+  auto go = [&](auto t) {
+    using T = decltype(t);
+    if (short_runs) hipLaunchKernelGGL((rotary_kernel<T, 2>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((rotary_kernel<T, 16 / T::BYTES>), grid, dim3(256), 0, st, a);
+  };
+  if (dtype == VIDKV_F16) go(TF16{});
+  else if (dtype == VIDKV_BF16) go(TBF16{});
+  else go(TF32{});
   return hipGetLastError();
 }
 
