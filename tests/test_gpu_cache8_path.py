@@ -202,3 +202,61 @@ def test_the_same_with_and_without_the_native_call_layer():
             vk._native = native
     for a, b in zip(*outs):
         assert torch.equal(a.nan_to_num(7.0) if a.is_floating_point() else a, b.nan_to_num(7.0) if b.is_floating_point() else b)
+
+
+def test_two_streams_at_once():
+    """Calls on two streams, each with its own cache and workspace, in turn and many deep: the results of calls by themselves."""
+    servers = [Server(i, torch.float16, seed=60 + i) for i in (0, 1)]
+    alone, jobs = [], []
+    for s in servers:
+        q, k, v = s.inputs(50)
+        q1, k1, v1 = s.inputs(1)
+        s.length = i32([CAP - 51] * B)
+        fill = torch.zeros((B, H, CAP - 51, 128), dtype=s.dtype, device=DEV)
+        vk.cache8_write(s.p, 0, s.buf, fill + 0.25, fill - 0.5, i32([0] * B))
+        jobs.append((q, k, v, s.positions(50), i32([50, 3, 0]), i32([CAP - 1, CAP - 48, CAP - 51])))
+        out, qt = torch.empty_like(q), torch.empty_like(q)
+        s.step(*jobs[-1][:4], out, qt, *jobs[-1][4:])
+        alone.append((out, s.buf.clone()))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in servers]
+    outs = [[] for _ in servers]
+    keep = []                                  # (what a side stream uses stays until both are done)
+    for turn in range(8):
+        for s, st, (q, k, v, pos, count, after), got in zip(servers, streams, jobs, outs):
+            out, qt = torch.empty_like(q), torch.empty_like(q)
+            keep.append((out, qt))
+            st.wait_stream(torch.cuda.current_stream())
+            vk.rotary(s.plan, pos, q, qt, stream=st)
+            vk.cache8_write(s.p, 0, s.buf, k, v, s.length, count, rotary=s.plan, positions=pos, stream=st)
+            vk.cache8_attention(s.p, 0, s.buf, qt, out, after, s.ws, q_count=count, stream=st)
+            got.append(out)
+    torch.cuda.synchronize()
+    for s, (out, buf), got in zip(servers, alone, outs):
+        assert all(torch.equal(out, o) for o in got) and torch.equal(s.buf, buf)
+
+
+@pytest.mark.parametrize("batch,heads", [(65535, 1), (1, 65535)])
+def test_the_most_sequences_and_heads(batch, heads):
+    p = vk.make_cache8(1, batch, heads, heads, 32)
+    buf = vk.alloc_bytes(vk.cache8_bytes(p), DEV)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(70)
+    k, v, q = (torch.randn((batch, heads, 1, 128), generator=g, device=DEV).half() for _ in range(3))
+    start = torch.zeros(batch, dtype=torch.int32, device=DEV)
+    vk.cache8_write(p, 0, buf, k, v, start)
+    back, out = torch.empty_like(v), torch.empty_like(q)
+    vk.cache8_read(p, 0, buf, start, None, back)
+    ws = vk.alloc_bytes(vk.cache8_workspace_bytes(p, 1))
+    vk.cache8_attention(p, 0, buf, q, out, start + 1, ws)
+    # one token: the weights are 1, and the result its value, rounded once more (2^-11 of it, and fp16's smallest)
+    assert ((out.double() - back.double()).abs() <= 2.0 ** -10 * back.double().abs() + 2.0 ** -24).all()
+    # half a step of the code, and of fp16
+    assert ((back.double() - v.double()).abs() <= v.double().abs().amax(dim=3, keepdim=True) * (0.5 / 127 + 2.0 ** -11)).all()
+    turned = torch.empty_like(q)
+    plan = vk.make_rotary(SECTIONS, theta=1e6)
+    if heads == 1:
+        vk.rotary(plan, torch.ones((3, batch, 1), dtype=torch.int32, device=DEV), q, turned)
+        vk.rotary(plan, torch.ones((3, batch, 1), dtype=torch.int32, device=DEV), turned, turned, inverse=True)
+        # there and back: two roundings of each of a pair's elements
+        assert ((turned.double() - q.double()).abs() <= 3 * 2.0 ** -11 * q.double().abs().amax(dim=3, keepdim=True)).all()
