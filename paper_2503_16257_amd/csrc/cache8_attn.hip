@@ -616,6 +616,7 @@ struct C8Plan {
   bool few;                    // waves share blocks (all rows fit one wave), else rows
   int waves;                   // few: a workgroup's
   int tiles, splits;
+  int most;                    // rows shared out: the splits that there can be
 };
 
 // Up to 48 rows a head are a wave's, and waves share the blocks.  One round of workgroups is best: each costs some 3 us before
@@ -639,10 +640,10 @@ static C8Plan c8_plan(const C8Geom& g, int n) {
     // merge's launch 4 us.  (112 rows of 256 heads over 1024 tokens: 31.0 us unsplit, 35.4 in two; 56 rows over 4096: 109 and 78;
     // 1372 rows of 32 heads over 512: 23 and 36.)
     const long long wgs = p.tiles * heads;
-    const int most = (int)std::min({(2 * cu + wgs - 1) / wgs, (g.nbc + 7LL) / 8, 256LL});
+    p.most = (int)std::min({(2 * cu + wgs - 1) / wgs, (g.nbc + 7LL) / 8, 256LL});
     const float alone = 0.8f + 0.1f * p.nt, beside = p.nt == 1 ? 1.0f : p.nt == 2 ? 1.25f : 1.65f;
     float least = 0.0f;
-    for (int k = 1; k <= std::max(most, 1); ++k) {
+    for (int k = 1; k <= p.most; ++k) {
       const float us = (float)g.nbc / k * (wgs * k <= cu ? alone : beside) +
                        (k > 1 ? 4.0f + (float)heads * (float)rows * k * (2 * 528 / 5e6f) : 0.0f);
       if (k == 1 || us < least) { least = us; p.splits = k; }
@@ -668,12 +669,14 @@ static size_t c8_parts(const C8Geom& g, long long rows, int splits) {
 size_t c8_attn_ws_need(const C8Geom& g, int n) { return c8_parts(g, (long long)n * g.rep, c8_plan(g, n).splits) + 256; }
 
 // ... and of the largest of the calls of up to n queries: fewer rows can mean more splits.  The plan changes with the
-// tiles of 16 or 192 rows; behind the last tile that is split there are no partials.
+// tiles of 16 or 192 rows, and within a tile more rows never mean more splits (a split costs each row the same).  Over the tiles the
+// splits do not fall steadily: where the workgroups pass the compute units a block takes longer, and a call is split again that was
+// not with fewer tiles.  They end where no more than one can be: two workgroups a compute unit without, or eight blocks in all.
 size_t c8_attn_ws_bytes(const C8Geom& g, int n) {
   size_t most = 0;
   for (long long q = 1; q <= n;) {
     const C8Plan p = c8_plan(g, (int)q);
-    if (p.nt == 3 && !p.few && p.splits == 1) break;
+    if (!p.few && p.most == 1) break;
     const long long rows = p.few ? 16LL * p.nt : 64LL * p.nt * p.tiles;          // the last of this plan
     const long long last = std::max(q, std::min<long long>(n, rows / g.rep));
     most = std::max(most, c8_parts(g, last * g.rep, p.splits));
