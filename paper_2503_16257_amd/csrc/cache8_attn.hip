@@ -16,6 +16,7 @@ namespace vidkv {
 
 constexpr float RISE = 8.0f, UP = 7.0f;
 constexpr float NONE = -1e30f;             // a maximum of nothing
+constexpr float FAR = 8.0f;                // a block's values are far below another's: by more than this factor
 
 struct C8Attn {
   View q, out;
@@ -400,7 +401,10 @@ __global__ __launch_bounds__(256, 2) void c8_many_kernel(C8Attn a, int tiles) {
       hold_order();
     }
   };
-  // the weights' sum over a block's tokens, as a product with ones: every element of the tile is it
+  // the weights' sum over a block's tokens, as a product with ones: every element of the tile is it.  P carries A_v, the
+  // weight does not: where A_v is far below the largest before it, P can lose bits in fp16, or vanish, whose weight is as large
+  // as any (a block of zeros has A_v = 2^-40).  Such a block's sum is taken in float32 (far_sums), and rv is 0 here; of
+  // others what fp16 loses is 2^-29 of the largest weight, a token.
   auto sums = [&](float rv) {
 #pragma unroll
     for (int t = 0; t < NT; ++t) r.l[t] = fmaf(mma(ones, p[t], f4{0.f, 0.f, 0.f, 0.f})[0], rv, r.l[t]);
@@ -449,6 +453,16 @@ __global__ __launch_bounds__(256, 2) void c8_many_kernel(C8Attn a, int tiles) {
 #pragma unroll
     for (int t = 0; t < NT; ++t) { ck[t] = r.cq[t] * km; off[t] = lv + UP - r.m[t]; }
   };
+  auto far_sums = [&](float rv) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      float sum = 0.0f, own = off[t];      // (not seen to be off: nothing of the common path is moved up here and kept)
+      asm volatile("" : "+v"(own));
+#pragma unroll
+      for (int k = 0; k < 8; ++k) sum += __builtin_amdgcn_exp2f(fmaf(s[t][k >> 2][k & 3], ck[t], own));
+      r.l[t] = fmaf(sum16(sum32(sum)), rv, r.l[t]);
+    }
+  };
   if (b0 < b1) {
     clear_dead(b0);
     put_v(b0, 0); put_v(b0, 1);
@@ -469,7 +483,7 @@ __global__ __launch_bounds__(256, 2) void c8_many_kernel(C8Attn a, int tiles) {
       for (int k = 0; k < 8; ++k) weight(t, k);
       p[t] = pn[t];
     }
-    float rv = __builtin_amdgcn_rcpf(vm);
+    float rv = __builtin_amdgcn_rcpf(vm), vmost = vm;          // the largest magnitude so far
     hand_over();
     // the weights of block i are there; block i + 1 is scored, and turned into weights between the products of block i
     for (int i = b0; i + 1 < b1; ++i) {
@@ -491,6 +505,11 @@ __global__ __launch_bounds__(256, 2) void c8_many_kernel(C8Attn a, int tiles) {
       lv = __log2f(vm);
       const bool rise = maxima(i + 1, km, lv);
       factors(km, lv);
+      vmost = fmaxf(vmost, vm);
+      if (vm * FAR < vmost) {
+        far_sums(rv);
+        rv = 0.0f;
+      }
       const Op(*o)[64] = ops[i & 1] + 8;
       n0 = o[0][lane];
       n1 = o[1][lane];
