@@ -418,7 +418,11 @@ vidkv_status vidkv_cache8_read(const vidkv_cache8 *p, int32_t layer, int32_t n_t
  * itself; with causal = 0 all.  A query that sees no token, and the rows from
  * q_count[b] on, get zeros.  Scores scale * q.k are held in fp32: a weight's
  * relative error is some 2^-24 of the largest of them (which is why they are to
- * stay below 2^24; beyond, weights are unspecified).
+ * stay below 2^24; beyond, weights are unspecified).  Weights are multiplied with
+ * the values in 11 bits, each rounded by at most 2^-11 of itself, and the sum that
+ * they are divided by is that of the rounded ones: equal values come out as they
+ * are, others to 2^-10 of Softmax(..) |V'| at most.  (Weights in a block whose values
+ * are an eighth of those of others or less are summed as they are.)
  *   q         in : [B, Hq, n_query, 128], fp16 or bf16
  *   out      out : likewise, of q's dtype (fp32 accumulation)
  *   length_dev in: [B] int32, taken as 0..capacity

@@ -82,8 +82,25 @@ __device__ __forceinline__ void load_block(Block& f, const uint8_t* kc, const ui
 // A row's denominator.  A query behind q_count went along where the others see every token: it has none.
 template <int NT>
 __device__ __forceinline__ float row_sum(const Rows<NT>& r, int t) {
-  const float l = sum16(sum32(r.l[t]));
-  return r.limit[t] > 0 ? l : 0.0f;
+  return r.limit[t] > 0 ? r.l[t] : 0.0f;
+}
+
+// The sum of a block's weights P over its tokens, in every lane, as a product with ones: of the weights as the other product
+// takes them, rounded, so that equal ones are rounded alike above and below.  P carries A_v, the weight does not: where A_v is
+// far below the largest before it, P can lose bits in fp16, or vanish, whose weight is as large as any (a block of zeros has
+// A_v = 2^-40).  Such a block's sum is taken in float32; of others what fp16 loses is 2^-29 of the largest weight, a token.
+__device__ __forceinline__ float sum_of(const Op& p) {
+  Op ones;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) ones.u[i] = 0x3c003c00u;
+  return mma(ones, p, f4{0.f, 0.f, 0.f, 0.f})[0];
+}
+__device__ __forceinline__ float far_sum(const f4 (&s)[2], float ck, float off) {
+  asm volatile("" : "+v"(off));            // (not seen to be off: nothing of the common path is moved up here and kept)
+  float sum = 0.0f;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) sum += __builtin_amdgcn_exp2f(fmaf(s[k >> 2][k & 3], ck, off));
+  return sum16(sum32(sum));
 }
 
 // Queries of 16 rows from `row0` on as operands; row = query * rep + head.
@@ -140,10 +157,10 @@ __device__ __forceinline__ void load_rows(Rows<NT>& r, const C8Attn& a, int b, i
 __device__ __forceinline__ void hold_order() { __builtin_amdgcn_sched_barrier(0); }
 
 // One block's tokens t0 .. t0 + 31 into the running sums; k(tt, j), v(m): its operands, tile of 16 tokens and 32 channels
-// of them, tile of 16 channels.  edge: some row does not see all of its tokens.
+// of them, tile of 16 channels.  edge: some row does not see all of its tokens.  far: its values are far below others.
 template <int NT, class K, class V>
-__device__ __forceinline__ void take_block(Rows<NT>& r, const K& k, const V& v, float km, float vm, bool edge, int t0,
-                                           int lane) {
+__device__ __forceinline__ void take_block(Rows<NT>& r, const K& k, const V& v, float km, float vm, bool edge, bool far,
+                                           int t0, int lane) {
   const int kb = lane >> 4;
   // operands are asked for two ahead of their products, and the order is held: left to itself the compiler asks for all of
   // them at once and has no registers left
@@ -161,7 +178,8 @@ __device__ __forceinline__ void take_block(Rows<NT>& r, const K& k, const V& v, 
     for (int t = 0; t < NT; ++t) s[t][g >> 1] = mma(o1, r.q[t][2 * (g & 1) + 1], s[t][g >> 1]);
     hold_order();
   }
-  const float lv = __log2f(vm), rv = __builtin_amdgcn_rcpf(vm);
+  const float lv = __log2f(vm);
+  float rv = __builtin_amdgcn_rcpf(vm);
   Op p[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
@@ -184,14 +202,9 @@ __device__ __forceinline__ void take_block(Rows<NT>& r, const K& k, const V& v, 
       for (int m = 0; m < 8; ++m) r.o[t][m] *= al;
     }
     const float off = lv + UP - r.m[t];
-    float sum = 0.0f;
+    if (far) r.l[t] = fmaf(far_sum(s[t], ck, off), rv, r.l[t]);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float e = __builtin_amdgcn_exp2f(fmaf(s[t][i >> 2][i & 3], ck, off));
-      sum += e;
-      p[t].v[i] = (_Float16)e;
-    }
-    r.l[t] = fmaf(sum, rv, r.l[t]);
+    for (int i = 0; i < 8; ++i) p[t].v[i] = (_Float16)__builtin_amdgcn_exp2f(fmaf(s[t][i >> 2][i & 3], ck, off));
     hold_order();
   }
 #pragma unroll
@@ -205,6 +218,9 @@ __device__ __forceinline__ void take_block(Rows<NT>& r, const K& k, const V& v, 
     for (int t = 0; t < NT; ++t) r.o[t][m + 1] = mma(o1, p[t], r.o[t][m + 1]);
     hold_order();
   }
+  if (far) rv = 0.0f;
+#pragma unroll
+  for (int t = 0; t < NT; ++t) r.l[t] = fmaf(sum_of(p[t]), rv, r.l[t]);
 }
 
 // The bytes of V codes (a lane group's eight tokens of a block, u0 and u1) of tokens that are there: n0 of the first four,
@@ -213,7 +229,7 @@ __device__ __forceinline__ uint32_t live(uint32_t u, int n) { return n >= 4 ? u 
 
 // A block out of a lane's registers.
 template <int NT, int CODE>
-__device__ __forceinline__ void take_codes(Rows<NT>& r, const Block& f, bool edge, int t0, int len, int lane) {
+__device__ __forceinline__ void take_codes(Rows<NT>& r, const Block& f, bool edge, bool far, int t0, int len, int lane) {
   const int n0 = len - t0 - 4 * (lane >> 4), n1 = n0 - 16;
   take_block<NT>(
       r, [&](int tt, int j) {
@@ -225,7 +241,7 @@ __device__ __forceinline__ void take_codes(Rows<NT>& r, const Block& f, bool edg
         if (CODE == 1 && edge) { u0 = live(u0, n0); u1 = live(u1, n1); }
         return decode8<CODE>(u0, u1);
       },
-      f.km, f.vm, edge, t0, lane);
+      f.km, f.vm, edge, far, t0, lane);
 }
 
 __device__ __forceinline__ void put_out(const C8Attn& a, int b, int h, int row, int c, const f4& v) {
@@ -261,9 +277,11 @@ __global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : NT < 3 ? 2 : 1) void c8_few
   if (b0 < b1) load_block(f, a.kc, a.vc, a.km, a.vm, head + b0, lane);      // (on its way while the queries are laid out)
   load_rows<NT>(r, a, b, h, 0, rows, len, nq, lane);
   if (b0 < b1) {
+    float vmost = 0.0f;                    // the largest magnitude so far
     for (int i = b0; i < b1; ++i) {
       if (i + 1 < b1) load_block(g, a.kc, a.vc, a.km, a.vm, head + i + 1, lane);
-      take_codes<NT, CODE>(r, f, (i + 1) * G > all, i * G, len, lane);
+      vmost = fmaxf(vmost, f.vm);
+      take_codes<NT, CODE>(r, f, (i + 1) * G > all, f.vm * FAR < vmost, i * G, len, lane);
       f = g;
     }
   }
@@ -375,9 +393,6 @@ __global__ __launch_bounds__(256, 2) void c8_many_kernel(C8Attn a, int tiles) {
   f4 s[NT][2];
   Op p[NT], n0, n1;
   float al[NT];
-  Op ones;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) ones.u[i] = 0x3c003c00u;
   // x of block i; between its products, what goes to LDS meanwhile: fill(0..3)
   auto scores = [&](int i, auto&& fill) {
     const Op(*o)[64] = ops[i & 1];
@@ -401,13 +416,10 @@ __global__ __launch_bounds__(256, 2) void c8_many_kernel(C8Attn a, int tiles) {
       hold_order();
     }
   };
-  // the weights' sum over a block's tokens, as a product with ones: every element of the tile is it.  P carries A_v, the
-  // weight does not: where A_v is far below the largest before it, P can lose bits in fp16, or vanish, whose weight is as large
-  // as any (a block of zeros has A_v = 2^-40).  Such a block's sum is taken in float32 (far_sums), and rv is 0 here; of
-  // others what fp16 loses is 2^-29 of the largest weight, a token.
+  // the weights' sums over a block's tokens; rv is 0 where far_sums had it
   auto sums = [&](float rv) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) r.l[t] = fmaf(mma(ones, p[t], f4{0.f, 0.f, 0.f, 0.f})[0], rv, r.l[t]);
+    for (int t = 0; t < NT; ++t) r.l[t] = fmaf(sum_of(p[t]), rv, r.l[t]);
   };
   // masks, and the maxima where they have to rise; true: o is to be multiplied by al
   auto maxima = [&](int i, float km, float lv) {
@@ -455,13 +467,7 @@ __global__ __launch_bounds__(256, 2) void c8_many_kernel(C8Attn a, int tiles) {
   };
   auto far_sums = [&](float rv) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      float sum = 0.0f, own = off[t];      // (not seen to be off: nothing of the common path is moved up here and kept)
-      asm volatile("" : "+v"(own));
-#pragma unroll
-      for (int k = 0; k < 8; ++k) sum += __builtin_amdgcn_exp2f(fmaf(s[t][k >> 2][k & 3], ck[t], own));
-      r.l[t] = fmaf(sum16(sum32(sum)), rv, r.l[t]);
-    }
+    for (int t = 0; t < NT; ++t) r.l[t] = fmaf(far_sum(s[t], ck[t], off[t]), rv, r.l[t]);
   };
   if (b0 < b1) {
     clear_dead(b0);

@@ -105,3 +105,24 @@ def test_blocks_far_apart(B, H, rep, n, cap, lens, causal, code):
     dtype = BF16 if code else F16
     q = torch.randn((B, H * rep, n, 128), generator=g, device=DEV).to(dtype)
     check(p, buf, q, attend(p, buf, q, lens, causal), lens, causal)
+
+
+@pytest.mark.parametrize("code", [0, 1])
+@pytest.mark.parametrize("rep,n,B,cap", [(16, 1, 300, 2048), (32, 1, 300, 2048), (16, 3, 300, 2048), (16, 8, 20, 2048),
+                                         (16, 12, 20, 256)])
+def test_equal_values_come_out_as_they_are(rep, n, B, cap, code):
+    """Values of 1 throughout: numerator and denominator are then the same sum of the same weights, whatever these are rounded
+    to.  Scores are 0 and one number a row up to 5.5 (2^8 of weight, which the maximum is not raised for) in turn of blocks.
+    Off by u (n + 600) <= 1.6e-4 before the rounding, less than the 2^-12 that fp16's 1 is rounded from."""
+    print(f"[case] equal rep={rep} n={n} B={B} cap={cap} code={code}", flush=True)
+    p, buf = empty(B, 1, rep, cap, code)
+    K = torch.zeros((B, 1, cap, 128), dtype=F16, device=DEV)
+    K[..., 0] = torch.arange(cap, device=DEV) // 32 % 2
+    vk.cache8_write(p, 0, buf, K, torch.ones_like(K), i32([0] * B))
+    q = torch.zeros((B, rep, n, 128), dtype=F16, device=DEV)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(72)
+    q[..., 0] = (5.5 / SCALE * torch.rand((B, rep, n), generator=g, device=DEV)).half()
+    out = attend(p, buf, q, [cap] * B)
+    print("  ", out.float().min().item(), out.float().max().item(), flush=True)
+    assert (out == 1.0).all()
