@@ -79,10 +79,11 @@ __device__ __forceinline__ void load_block(Block& f, const uint8_t* kc, const ui
   f.vm = vm[blk];
 }
 
-// A row's denominator.  A query behind q_count went along where the others see every token: it has none.
+// A row's maximum and denominator.  A query behind q_count went along where the others see every token: it has none, and
+// whatever it is (an infinity times a weight of none would be no number) it gives zeros.
 template <int NT>
-__device__ __forceinline__ float row_sum(const Rows<NT>& r, int t) {
-  return r.limit[t] > 0 ? r.l[t] : 0.0f;
+__device__ __forceinline__ f2 row_stats(const Rows<NT>& r, int t) {
+  return r.limit[t] > 0 ? f2{r.m[t], r.l[t]} : f2{NONE, 0.0f};
 }
 
 // The sum of a block's weights P over its tokens, in every lane, as a product with ones: of the weights as the other product
@@ -290,9 +291,9 @@ __global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : NT < 3 ? 2 : 1) void c8_few
   __shared__ float sm[W][16], sl[W][16];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    const float l = row_sum(r, t);
+    const f2 ml = row_stats(r, t);
     if (t > 0) __syncthreads();
-    if (kb == 0) { sm[w][x] = r.m[t]; sl[w][x] = l; }
+    if (kb == 0) { sm[w][x] = ml[0]; sl[w][x] = ml[1]; }
 #pragma unroll
     for (int m = 0; m < 8; ++m) so[w][x][4 * m + kb] = r.o[t][m];
     __syncthreads();
@@ -557,15 +558,15 @@ __global__ __launch_bounds__(256, 2) void c8_many_kernel(C8Attn a, int tiles) {
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const int row = row0 + 16 * t + x;
-    const float l = r.limit[t] > 0 ? r.l[t] : 0.0f;
+    const f2 ml = row_stats(r, t);
     if (row >= rows) continue;
     if (a.po) {
       const size_t at = (((size_t)b * a.H + h) * rows + row) * a.splits + sp;
 #pragma unroll
       for (int m = 0; m < 8; ++m) reinterpret_cast<f4*>(a.po)[at * (D / 4) + 4 * m + kb] = r.o[t][m];
-      if (kb == 0) { a.pml[2 * at] = r.m[t]; a.pml[2 * at + 1] = l; }
+      if (kb == 0) { a.pml[2 * at] = ml[0]; a.pml[2 * at + 1] = ml[1]; }
     } else {
-      const float f = l != 0.0f ? a.inv_level / l : 0.0f;
+      const float l = ml[1], f = l != 0.0f ? a.inv_level / l : 0.0f;
 #pragma unroll
       for (int m = 0; m < 8; ++m) put_out(a, b, h, row, 16 * m + 4 * kb, l != 0.0f ? r.o[t][m] * f : f4{0.f, 0.f, 0.f, 0.f});
     }

@@ -126,3 +126,23 @@ def test_equal_values_come_out_as_they_are(rep, n, B, cap, code):
     out = attend(p, buf, q, [cap] * B)
     print("  ", out.float().min().item(), out.float().max().item(), flush=True)
     assert (out == 1.0).all()
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("rep,n", [(4, 3), (16, 2), (2, 40), (7, 60)])
+def test_infinite_queries_behind_the_count_give_zeros(rep, n, dtype):
+    """Keys above zero in the channel where such a query is infinite: its scores are infinite, not NaN."""
+    for cap, causal in ((320, True), (320, False), (6272, True)):
+        print(f"[case] behind the count rep={rep} n={n} cap={cap} {dtype}", flush=True)
+        p, buf = empty(1, 1, rep, cap, 0)
+        g = torch.Generator(device=DEV)
+        g.manual_seed(74)
+        K, V = (torch.randn((1, 1, cap, 128), generator=g, device=DEV) for _ in range(2))
+        K[..., 0] = K[..., 0].abs() + 2
+        vk.cache8_write(p, 0, buf, K.to(dtype), V.to(dtype), i32([0]))
+        q = torch.randn((1, rep, n, 128), generator=g, device=DEV).to(dtype)
+        q[:, :, n - 1:] = 0
+        want = attend(p, buf, q, [cap], causal, [n - 1])
+        q[:, :, n - 1:, 0] = float("inf")
+        got = attend(p, buf, q, [cap], causal, [n - 1])
+        assert (got[:, :, n - 1:] == 0).all() and torch.equal(got, want)
