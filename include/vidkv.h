@@ -406,7 +406,8 @@ vidkv_status vidkv_cache8_write(const vidkv_cache8 *p, int32_t layer, int32_t n_
 
 /* Reads tokens start[b] .. start[b] + n_tokens - 1 of one layer back as values
  * (fp16, bf16 or fp32; either output may be NULL).  Tokens outside
- * 0..capacity-1 come as zeros; those never written are unspecified. */
+ * 0..capacity-1 come as zeros; those never written are unspecified, or zeros where
+ * the buffer was cleared. */
 vidkv_status vidkv_cache8_read(const vidkv_cache8 *p, int32_t layer, int32_t n_tokens,
                                const int32_t *start_dev, const void *cache_dev,
                                size_t cache_bytes, const vidkv_view *K, const vidkv_view *V,
@@ -423,6 +424,8 @@ vidkv_status vidkv_cache8_read(const vidkv_cache8 *p, int32_t layer, int32_t n_t
  * they are divided by is that of the rounded ones: equal values come out as they
  * are, others to 2^-10 of Softmax(..) |V'| at most.  (Weights in a block whose values
  * are an eighth of those of others or less are summed as they are.)
+ * Tokens that were never written are unspecified, as in reading, but in a cleared
+ * buffer they are zeros (a sequence padded on the left), and take part as such.
  *   q         in : [B, Hq, n_query, 128], fp16 or bf16
  *   out      out : likewise, of q's dtype (fp32 accumulation)
  *   length_dev in: [B] int32, taken as 0..capacity

@@ -79,6 +79,10 @@ __device__ __forceinline__ void load_block(Block& f, const uint8_t* kc, const ui
   f.vm = vm[blk];
 }
 
+// A block's magnitude as the sums take it.  A cleared buffer's, of a block that was never written, is zero: tokens of zeros, as
+// they are read back, and no quotient by it.
+__device__ __forceinline__ float held(float mag) { return fmaxf(mag, C8_LEAST); }
+
 // A row's maximum and denominator.  A query behind q_count went along where the others see every token: it has none, and
 // whatever it is (an infinity times a weight of none would be no number) it gives zeros.
 template <int NT>
@@ -281,6 +285,8 @@ __global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : NT < 3 ? 2 : 1) void c8_few
     float vmost = 0.0f;                    // the largest magnitude so far
     for (int i = b0; i < b1; ++i) {
       if (i + 1 < b1) load_block(g, a.kc, a.vc, a.km, a.vm, head + i + 1, lane);
+      f.km = held(f.km);
+      f.vm = held(f.vm);
       vmost = fmaxf(vmost, f.vm);
       take_codes<NT, CODE>(r, f, (i + 1) * G > all, f.vm * FAR < vmost, i * G, len, lane);
       f = g;
@@ -385,7 +391,7 @@ __global__ __launch_bounds__(256, 2) void c8_many_kernel(C8Attn a, int tiles) {
   float km = 1.0f, vm = 1.0f;
   if (b0 < b1) {
     ask_k(b0);
-    gk0 = gk; km = gkm; vm = gvm;
+    gk0 = gk; km = held(gkm); vm = held(gvm);
     ask_v(b0);
     ask_k(b0 + 1);
   }
@@ -498,7 +504,7 @@ __global__ __launch_bounds__(256, 2) void c8_many_kernel(C8Attn a, int tiles) {
       // turns of a block each: 322 -> 311 us)
       if ((i ^ (blockIdx.x >> 8)) & 1) __builtin_amdgcn_s_setprio(1);
       else __builtin_amdgcn_s_setprio(0);
-      km = kn; vm = vn;
+      km = held(kn); vm = held(vn);
       kn = gkm; vn = gvm;
       clear_dead(i + 1);
       scores(i + 1, [&](int g) {

@@ -128,6 +128,23 @@ def test_equal_values_come_out_as_they_are(rep, n, B, cap, code):
     assert (out == 1.0).all()
 
 
+@pytest.mark.parametrize("code", [0, 1])
+@pytest.mark.parametrize("rep,n", [(4, 1), (4, 9), (2, 40), (7, 40)])
+def test_cleared_blocks_are_tokens_of_zeros(rep, n, code):
+    """A cleared buffer whose first 69 tokens were never written: a left-padded sequence.  They come back as zeros, and the
+    attention takes them as such."""
+    for cap in (128, 4096):
+        print(f"[case] cleared rep={rep} n={n} cap={cap} code={code}", flush=True)
+        p, buf = empty(1, 1, rep, cap, code, fill=0)
+        g = torch.Generator(device=DEV)
+        g.manual_seed(73)
+        K, V = (torch.randn((1, 1, cap - 69, 128), generator=g, device=DEV).half() for _ in range(2))
+        vk.cache8_write(p, 0, buf, K, V, i32([69]))
+        q = torch.randn((1, rep, n, 128), generator=g, device=DEV).half()
+        for lens, causal in (([cap], False), ([110], True), ([69], False), ([64], True)):
+            check(p, buf, q, attend(p, buf, q, lens, causal), lens, causal)
+
+
 @pytest.mark.parametrize("dtype", [F16, BF16])
 @pytest.mark.parametrize("rep,n", [(4, 3), (16, 2), (2, 40), (7, 60)])
 def test_infinite_queries_behind_the_count_give_zeros(rep, n, dtype):
