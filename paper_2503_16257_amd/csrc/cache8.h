@@ -100,7 +100,7 @@ struct TF16 {
   }
   static __device__ __forceinline__ u32x4 pack8(f8v v) { return __builtin_bit_cast(u32x4, __builtin_convertvector(v, h8)); }
   static __device__ __forceinline__ float of_bits(uint32_t u) { return (float)__builtin_bit_cast(_Float16, (uint16_t)u); }
-  static constexpr float MOST = 65504.0f;
+  static constexpr uint16_t TOP = 0x7bff;            // bits of the largest magnitude that goes into a block: of the type
 };
 
 struct TBF16 {
@@ -129,7 +129,7 @@ struct TBF16 {
   }
   static __device__ __forceinline__ u32x4 pack8(f8v v) { return __builtin_bit_cast(u32x4, __builtin_convertvector(v, b8)); }
   static __device__ __forceinline__ float of_bits(uint32_t u) { return __uint_as_float(u << 16); }
-  static constexpr float MOST = 3.39e38f;
+  static constexpr uint16_t TOP = 0x5380;            // ... C8_MOST
 };
 
 struct TF32 {
@@ -211,16 +211,10 @@ __device__ __forceinline__ float units(float x, float up, float A, float rA) {
   return fmaf(fmaf(-q, A, n), rA, q);
 }
 
-// Four values in the code's units as four codes; CLAMP: where a value may be beyond the largest code (a magnitude that was
-// held at its upper bound, which fp16 does not reach).  int8: 1.5 * 2^23 added, which rounds to an integer, ties to even, and
-// leaves it in the low byte.
-template <int CODE, bool CLAMP>
+// Four values in the code's units as four codes.  int8: 1.5 * 2^23 added, which rounds to an integer, ties to even, and leaves it in
+// the low byte.
+template <int CODE>
 __device__ __forceinline__ uint32_t code4(float a, float b, float c, float d) {
-  constexpr float M = kLevel<CODE>;
-  if constexpr (CLAMP) {
-    a = __builtin_amdgcn_fmed3f(a, -M, M); b = __builtin_amdgcn_fmed3f(b, -M, M);
-    c = __builtin_amdgcn_fmed3f(c, -M, M); d = __builtin_amdgcn_fmed3f(d, -M, M);
-  }
   if constexpr (CODE == 0) {
     constexpr float R = 12582912.0f;
     const uint32_t lo = __builtin_amdgcn_perm(__float_as_uint(b + R), __float_as_uint(a + R), 0x0c0c0400u);

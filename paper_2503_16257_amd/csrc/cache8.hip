@@ -4,6 +4,7 @@
 // x / A.  2 bytes in and 1 out an element (1 in and 2 or 4 out on the way back): bound by HBM; one token a sequence: by
 // the chain start -> row -> maximum over the workgroup -> code.
 #include "cache8.h"
+#include <algorithm>
 
 namespace vidkv {
 
@@ -39,8 +40,15 @@ __device__ __forceinline__ us2 wave_max(us2 v) {
   return __builtin_elementwise_max(__builtin_bit_cast(us2, r0), __builtin_bit_cast(us2, r1));
 }
 
-// A block's magnitude as it is stored: never zero, and bounded so that no product with it leaves float's range.
+// A block's magnitude as it is stored: never zero, and bounded, as its elements are, so that no product of them leaves float's range.
 __device__ __forceinline__ float bounded(float a) { return fminf(fmaxf(a, C8_LEAST), C8_MOST); }
+
+// Two elements held to the largest magnitude that goes into a block.
+template <class T>
+__device__ __forceinline__ uint32_t held(uint32_t u) {
+  const us2 m = __builtin_elementwise_min(__builtin_bit_cast(us2, u & 0x7fff7fffu), us2{T::TOP, T::TOP});
+  return (u & 0x80008000u) | __builtin_bit_cast(uint32_t, m);
+}
 
 constexpr int FEW = 8;                     // new tokens of a block whose sines are shared out
 
@@ -76,7 +84,6 @@ __global__ __launch_bounds__(256) void c8_write_kernel(C8Write a) {
   const bool begun = t0 < start;           // live tokens stand before the new ones
   const bool whole = lo == t0 && hi == t0 + G;
   constexpr float LV = kLevel<CODE>;
-  constexpr bool CLAMP = T::MOST > C8_MOST;
 
   // keys
   const int kt = t0 + (tid >> 3), u = tid & 7;
@@ -147,30 +154,38 @@ __global__ __launch_bounds__(256) void c8_write_kernel(C8Write a) {
       }
       turn_runs<8>(x, y, a.rot.adjacent, co, si);
     }
-  } else {
-    x = T::widen(rx); y = T::widen(ry);
   }
   ko = bounded(ko); vo = bounded(vo);
 
-  // magnitudes of 16-bit numbers compare as integers do, two at a time
-  us2 vm{0, 0}, km{0, 0};
-#pragma unroll
-  for (int j = 0; j < 8; ++j) vm = __builtin_elementwise_max(vm, __builtin_bit_cast(us2, v[j] & 0x7fff7fffu));
   u32x4 bx = __builtin_bit_cast(u32x4, rx), by = __builtin_bit_cast(u32x4, ry);
-  if constexpr (ROT) {                     // rounded to the tensor's type, as the rotation by itself leaves them
-    bx = T::pack8(x); by = T::pack8(y);
-    x = T::widen(__builtin_bit_cast(typename T::Run, bx));
-    y = T::widen(__builtin_bit_cast(typename T::Run, by));
-  }
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    km = __builtin_elementwise_max(km, __builtin_elementwise_max(__builtin_bit_cast(us2, bx[e] & 0x7fff7fffu),
-                                                                 __builtin_bit_cast(us2, by[e] & 0x7fff7fffu)));
-  us2 most = wave_max(us2{max(km[0], km[1]), max(vm[0], vm[1])});
+  if constexpr (ROT) { bx = T::pack8(x); by = T::pack8(y); }   // rounded to the tensor's type, as the rotation by itself leaves them
+  // magnitudes of 16-bit numbers compare as integers do, two at a time
   __shared__ us2 red[4];
-  if (lane == 0) red[w] = most;
-  __syncthreads();
-  most = __builtin_elementwise_max(__builtin_elementwise_max(red[0], red[1]), __builtin_elementwise_max(red[2], red[3]));
+  auto largest = [&] {
+    us2 vm{0, 0}, km{0, 0};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) vm = __builtin_elementwise_max(vm, __builtin_bit_cast(us2, v[j] & 0x7fff7fffu));
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      km = __builtin_elementwise_max(km, __builtin_elementwise_max(__builtin_bit_cast(us2, bx[e] & 0x7fff7fffu),
+                                                                   __builtin_bit_cast(us2, by[e] & 0x7fff7fffu)));
+    const us2 most = wave_max(us2{std::max(km[0], km[1]), std::max(vm[0], vm[1])});
+    if (lane == 0) red[w] = most;
+    __syncthreads();
+    const us2 all = __builtin_elementwise_max(__builtin_elementwise_max(red[0], red[1]), __builtin_elementwise_max(red[2], red[3]));
+    return __builtin_bit_cast(us2, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, all)));
+  };
+  us2 most = largest();
+  if (max(most[0], most[1]) > T::TOP) {    // (the whole workgroup's: all of it comes here or none)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = held<T>(v[j]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { bx[e] = held<T>(bx[e]); by[e] = held<T>(by[e]); }
+    __syncthreads();                       // red has been read
+    most = largest();
+  }
+  x = T::widen(__builtin_bit_cast(typename T::Run, bx));
+  y = T::widen(__builtin_bit_cast(typename T::Run, by));
   float ka = bounded(T::of_bits(most[0])), va = bounded(T::of_bits(most[1]));
   if (begun) { ka = fmaxf(ka, ko); va = fmaxf(va, vo); }
   const float rk = __builtin_amdgcn_rcpf(ka), rv = __builtin_amdgcn_rcpf(va);
@@ -180,15 +195,15 @@ __global__ __launch_bounds__(256) void c8_write_kernel(C8Write a) {
   auto again = [](uint32_t c, float old, float A, float rA) {
     h2 l, g;
     decode4<CODE>(c, &l, &g);
-    return code4<CODE, false>(units((float)l[0], old, A, rA), units((float)l[1], old, A, rA), units((float)g[0], old, A, rA),
+    return code4<CODE>(units((float)l[0], old, A, rA), units((float)l[1], old, A, rA), units((float)g[0], old, A, rA),
                        units((float)g[1], old, A, rA));
   };
   if (knew) {
     uint2 p, q;
-    p.x = code4<CODE, CLAMP>(units(x[0], LV, ka, rk), units(x[1], LV, ka, rk), units(x[2], LV, ka, rk), units(x[3], LV, ka, rk));
-    p.y = code4<CODE, CLAMP>(units(x[4], LV, ka, rk), units(x[5], LV, ka, rk), units(x[6], LV, ka, rk), units(x[7], LV, ka, rk));
-    q.x = code4<CODE, CLAMP>(units(y[0], LV, ka, rk), units(y[1], LV, ka, rk), units(y[2], LV, ka, rk), units(y[3], LV, ka, rk));
-    q.y = code4<CODE, CLAMP>(units(y[4], LV, ka, rk), units(y[5], LV, ka, rk), units(y[6], LV, ka, rk), units(y[7], LV, ka, rk));
+    p.x = code4<CODE>(units(x[0], LV, ka, rk), units(x[1], LV, ka, rk), units(x[2], LV, ka, rk), units(x[3], LV, ka, rk));
+    p.y = code4<CODE>(units(x[4], LV, ka, rk), units(x[5], LV, ka, rk), units(x[6], LV, ka, rk), units(x[7], LV, ka, rk));
+    q.x = code4<CODE>(units(y[0], LV, ka, rk), units(y[1], LV, ka, rk), units(y[2], LV, ka, rk), units(y[3], LV, ka, rk));
+    q.y = code4<CODE>(units(y[4], LV, ka, rk), units(y[5], LV, ka, rk), units(y[6], LV, ka, rk), units(y[7], LV, ka, rk));
     *pk0 = p;
     *pk1 = q;
   } else if (kt < start && ka > ko) {      // (only in a begun block)
@@ -204,7 +219,7 @@ __global__ __launch_bounds__(256) void c8_write_kernel(C8Write a) {
     float f[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) f[j] = units(T::widen2(v[j])[i], LV, va, rv);
-    n[i] = uint2{code4<CODE, CLAMP>(f[0], f[1], f[2], f[3]), code4<CODE, CLAMP>(f[4], f[5], f[6], f[7])};
+    n[i] = uint2{code4<CODE>(f[0], f[1], f[2], f[3]), code4<CODE>(f[4], f[5], f[6], f[7])};
   }
   const bool upper = lane & 8;
   const uint2 give = upper ? n[0] : n[1], keep = upper ? n[1] : n[0];
