@@ -43,11 +43,13 @@ __device__ __forceinline__ us2 wave_max(us2 v) {
 // A block's magnitude as it is stored: never zero, and bounded, as its elements are, so that no product of them leaves float's range.
 __device__ __forceinline__ float bounded(float a) { return fminf(fmaxf(a, C8_LEAST), C8_MOST); }
 
-// Two elements held to the largest magnitude that goes into a block.
+// Two elements held to the largest magnitude that goes into a block: an infinity is the type's largest number, a NaN a zero,
+// so that no code is one (a weight of zero times it would be a NaN in rows that do not see its token).
 template <class T>
 __device__ __forceinline__ uint32_t held(uint32_t u) {
-  const us2 m = __builtin_elementwise_min(__builtin_bit_cast(us2, u & 0x7fff7fffu), us2{T::TOP, T::TOP});
-  return (u & 0x80008000u) | __builtin_bit_cast(uint32_t, m);
+  const uint32_t a = u & 0x7fffu, b = u >> 16 & 0x7fffu, lo = a > T::INF ? 0 : min(a, (uint32_t)T::TOP),
+                 hi = b > T::INF ? 0 : min(b, (uint32_t)T::TOP);
+  return (u & 0x80008000u) | lo | hi << 16;
 }
 
 constexpr int FEW = 8;                     // new tokens of a block whose sines are shared out
