@@ -102,10 +102,10 @@ hipError_t launch_rotary(const vidkv_rotary* r, int inverse, int B, int n, const
   const bool short_runs = (long long)a.rows * heads <= 2048;
   const int run = short_runs ? 2 : 16 / dtype_bytes(dtype), tpw = 256 / (r->head_dim / (2 * run));
   const int tiles = (a.rows + tpw - 1) / tpw;
-  // two heads a thread where that leaves a workgroup a compute unit or so (32 heads x 6272 tokens in bf16, one, two, four and
-  // eight heads: 29.1, 22.8, 22.3, 23.7 us; x 1000: 6.4, 5.6, 5.7, 7.0; x 64 of one token: 4.5, 4.7, 4.7, 6.1); a thread of
-  // float32 makes half as many sines (3 x 4097 tokens of 32 heads: 46.5, 47.9, 49.4, 50.9)
-  a.per = dtype != VIDKV_F32 && !short_runs && (long long)tiles * heads >= 256 ? 2 : 1;
+  // two heads a thread where that leaves a workgroup for every second compute unit (32 heads x 6272 tokens in bf16, one, two,
+  // four and eight heads: 29.1, 22.8, 22.3, 23.7 us; x 1000: 6.4, 5.6, 5.7, 7.0; x 64 of one token: 4.5, 4.7, 4.7, 6.1); a thread
+  // of float32 makes half as many sines (3 x 4097 tokens of 32 heads: 46.5, 47.9, 49.4, 50.9)
+  a.per = dtype != VIDKV_F32 && !short_runs && (long long)tiles * heads >= device_cu_count() ? 2 : 1;
   const dim3 grid(tiles, (heads + a.per - 1) / a.per);
   auto go = [&](auto t) {
     using T = decltype(t);
