@@ -351,8 +351,9 @@ vidkv_status vidkv_rotary_init(vidkv_rotary *rot, int32_t head_dim, int32_t rot_
  *   k, k_out       : [batch, n_k_heads, ...] likewise, of q's dtype
  *   inverse        : 0 turns by +angle; 1 by -angle: undoes the rotation, and is
  *                    its backward pass (gradients of y in, gradients of x out)
- * Computed in fp32 (angles to 2^-33 turns), rounded once.  batch * n_tokens is at
- * most 2^26 (else VIDKV_ESHAPE). */
+ * Computed in fp32 (angles within the nearest quarter turn to 24 bits: 2^-28 turns,
+ * at any position), rounded once.  batch * n_tokens is at most 2^26 (else
+ * VIDKV_ESHAPE). */
 vidkv_status vidkv_rotary_apply(const vidkv_rotary *rot, int32_t inverse, int32_t batch,
                                 int32_t n_tokens, const int32_t *pos_dev, int32_t n_q_heads,
                                 const vidkv_view *q, const vidkv_view *q_out, int32_t n_k_heads,
@@ -428,7 +429,9 @@ vidkv_status vidkv_cache8_read(const vidkv_cache8 *p, int32_t layer, int32_t n_t
  * are an eighth of those of others or less are summed as they are.)
  * Tokens that were never written are unspecified, as in reading, but in a cleared
  * buffer they are zeros (a sequence padded on the left), and take part as such.
- *   q         in : [B, Hq, n_query, 128], fp16 or bf16
+ *   q         in : [B, Hq, n_query, 128], fp16 or bf16; what a bf16 row holds is
+ *                  taken to 2^-39 of its largest element, and q times the scale is to
+ *                  stay below 2^64
  *   out      out : likewise, of q's dtype (fp32 accumulation)
  *   length_dev in: [B] int32, taken as 0..capacity
  *   q_count_dev in: [B] int32, taken as 0..n_query; NULL: n_query

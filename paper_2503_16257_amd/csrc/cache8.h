@@ -151,7 +151,8 @@ struct TF32 {
 // ---- rotation -------------------------------------------------------------------------------
 // cos and sin of 2 pi t / 2^64 for t = position * turn modulo 2^64: the nearest quarter turn is taken
 // off exactly, the rest y, at most pi/4, goes through the two Taylor sums (behind them: y^11/11! = 1.8e-9,
-// y^12/12! = 1.2e-10).  Its top 32 bits make y exact to 2^-33 turns, and a float keeps 24 bits of it.
+// y^12/12! = 1.2e-10).  Its top 32 bits are taken, 2^-32 turns at most are cut off, and a float keeps 24 bits of them: 2^-28 turns
+// at an eighth of a turn, less of smaller angles.
 __device__ __forceinline__ void turn_cos_sin(int pos, uint64_t turn, float* c, float* s) {
   const uint64_t t = (uint64_t)(int64_t)pos * turn;
   const uint32_t q = (uint32_t)((t + (1ull << 61)) >> 62);

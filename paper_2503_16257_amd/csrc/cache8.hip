@@ -65,7 +65,7 @@ __device__ __forceinline__ uint32_t lane_xor8(uint32_t v) {
 // What a workgroup waits for - rows, positions, a begun block's magnitudes and codes - is asked for as soon as its block
 // is known.  8 x 4 heads x 12544 tokens in fp16: 67 us for 308 MB, 4.6 TB/s; the vector units are the second bound, 9
 // instructions an element of which the exact quotient is 4 (with a branch a row, values in 8-byte stores at every second place
-// and maxima in float32: 84 us).  One token of 64 sequences, turned: 5.3 us.  grid (blocks a sequence can reach, H, B).
+// and maxima in float32: 84 us).  One token of 64 sequences, turned: 5.5 us.  grid (blocks a sequence can reach, H, B).
 template <class T, int CODE, bool ROT>
 __global__ __launch_bounds__(256) void c8_write_kernel(C8Write a) {
   // (all arguments in one round trip; left to itself the compiler asks for each where it is used)

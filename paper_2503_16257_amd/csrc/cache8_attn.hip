@@ -6,8 +6,9 @@
 //   P = 2^(x ck + log2 A_v - m),  o[channel][row] += sum_t V[t][channel] P[t][row],  l += sum_t P / A_v
 // with ck = A_k * scale * log2 e / level: the magnitude of a block's values goes into the exponent, where it costs an
 // addition a row, and the accumulators stay in the codes' units.  out = o / (l level).  The maximum m of
-// x ck + log2 A_v is a row's; it is raised only when a score exceeds it by 2^RISE, and P stays below 2^(RISE + UP) = 2^15, so
-// that a P of 2^-29 of the largest still has fp16's 11 bits.
+// x ck + log2 A_v is a row's; it is raised only when a score exceeds it by 2^RISE, and P stays below 2^(RISE + UP) = 2^15.
+// P is rounded to fp16, 11 bits down to 2^-14: down to 2^-21 of the largest where the maximum has just been raised (the largest is
+// 2^UP then), 2^-29 where it is about to be; below, what is lost is 2^-32 of the largest at most.
 // bf16 queries become fp16 operands under a power of two of their own row.
 #include "cache8.h"
 #include <algorithm>
@@ -94,6 +95,8 @@ __device__ __forceinline__ f2 row_stats(const Rows<NT>& r, int t) {
 // takes them, rounded, so that equal ones are rounded alike above and below.  P carries A_v, the weight does not: where A_v is
 // far below the largest before it, P can lose bits in fp16, or vanish, whose weight is as large as any (a block of zeros has
 // A_v = 2^-40).  Such a block's sum is taken in float32; of others what fp16 loses is 2^-29 of the largest weight, a token.
+// (Many queries, vector units the bound: float32 for every second block 271 -> 306 us, for all of them 348; the look alone 3.
+// Few queries, memory the bound: the same times, 40 rows 25.5 -> 25.7 and 26.8.)
 __device__ __forceinline__ float sum_of(const Op& p) {
   Op ones;
 #pragma unroll
@@ -336,8 +339,8 @@ __global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : NT < 3 ? 2 : 1) void c8_few
 // 8.6 cycles, half a conversion, half a maximum; the decoding: 40).  So: the more rows a wave, the fewer decodings and LDS
 // reads a row - 48 rows are what 256 registers hold, two waves a SIMD (32 rows, three waves: 410 us where 48 took 352) -
 // the weights of a block are made between the products of the block before, the decoding between those of the scores, and
-// the denominators are products with ones.  196 queries x 28 heads over 98196 tokens, int8: 262 us, 1.05 PFLOP/s (1.18 with
-// the rows that pad the last tile); 6272 over themselves, causal: 270 us, 1.04.  On the way there: each wave decoding for
+// the denominators are products with ones.  196 queries x 28 heads over 98196 tokens, int8: 266 us, 1.04 PFLOP/s (1.16 with
+// the rows that pad the last tile); 6272 over themselves, causal: 274 us, 1.03.  On the way there: each wave decoding for
 // itself from memory 902 and 750; the weights in a phase of their own 340 and 350; eight waves to a workgroup, half the
 // decoding each: the same.  32 x 32 x 16 products, which cost the vector units less, with 32 rows a wave: 460 and 355.
 // grid (tiles of rows x splits x B x H), heads fastest: the tiles that see most come first, and what shares a head's
@@ -651,9 +654,13 @@ struct C8Plan {
   int most;                    // rows shared out: the splits that there can be
 };
 
-// Up to 48 rows a head are a wave's, and waves share the blocks.  One round of workgroups is best: each costs some 3 us before
-// its first product and its partials as long behind the last (196000 tokens, 4 heads: 40.8 us with a workgroup a compute
-// unit, 41.5 with two, 44.9 with four; 16 sequences of up to 6001 tokens, 40 rows: 23.6, 28.6, 38.2).
+// Up to 48 rows a head are a wave's, and waves share the blocks; more are shared out over waves, which walk the blocks together (e4m3,
+// 24, 32, 40 and 48 rows of 4 heads, this way and that: one sequence of 98208 tokens 24.6, 25.2, 27.5, 27.3 and 32.1, 32.7, 33.2,
+// 33.9 us; 16 of up to 6001 19.6, 19.2, 23.9, 25.0 and 26.9, 25.2, 26.6, 28.4; 64 of 6016 78, 80, 91, 89 and 100, 101, 103, 104; a
+// fourth tile a wave, at 56 and 64 rows: 32.3, 33.0 against 35.0, 37.6; 30.6, 30.1 against 28.7, 28.5; 102, 104 against 107, 110).
+// Waves that share blocks do best in one round of workgroups: each costs some 3 us before its first product and its partials as long
+// behind the last (196000 tokens, 4 heads: 40.8 us with a workgroup a compute unit, 42.1 with two, 45.1 with four; 16 sequences of up to
+// 6001 tokens, 40 rows: 23.8, 29.3, 38.8).
 // Where the heads are three quarters of the compute units or more, for caches of up to 2048 tokens half of them, a workgroup
 // of twelve waves takes a head and there is no merge (64 x 4 heads of 512 tokens 13.2 -> 8.9 us, of 8192 113 -> 91; 1024 heads of
 // 2048 tokens 109 -> 100, but of 384 tokens 19 -> 29; 128 heads of 2048 tokens 16.5 -> 15.1, of 2048 to 4096 23.2 -> 27.8),
