@@ -429,9 +429,8 @@ vidkv_status vidkv_cache8_read(const vidkv_cache8 *p, int32_t layer, int32_t n_t
  * are an eighth of those of others or less are summed as they are.)
  * Tokens that were never written are unspecified, as in reading, but in a cleared
  * buffer they are zeros (a sequence padded on the left), and take part as such.
- *   q         in : [B, Hq, n_query, 128], fp16 or bf16; what a bf16 row holds is
- *                  taken to 2^-39 of its largest element, and q times the scale is to
- *                  stay below 2^64
+ *   q         in : [B, Hq, n_query, 128], fp16 or bf16 (the elements of a bf16 row
+ *                  are taken to 2^-39 of its largest)
  *   out      out : likewise, of q's dtype (fp32 accumulation)
  *   length_dev in: [B] int32, taken as 0..capacity
  *   q_count_dev in: [B] int32, taken as 0..n_query; NULL: n_query

@@ -150,9 +150,10 @@ __device__ __forceinline__ void load_rows(Rows<NT>& r, const C8Attn& a, int b, i
 #pragma unroll
       for (int j = 0; j < 4; ++j) r.q[t][j].v = __builtin_convertvector(v[j] * f, h8);
     }
-    // (bounded so that its products with a magnitude and with a score neither vanish - a masked score times it would be no
-    // number - nor leave float's range; beyond the bounds a row's weights are equal, or one of them all)
-    r.cq[t] = fminf(fmaxf(a.scale2 * back, 0x1p-86f), 0x1p49f);
+    // (bounded so that its products with a magnitude, 2^-40..2^40, neither vanish nor leave float's range: a masked score times
+    // them, or one of zero, would be no number.  Below the bound a row's weights are equal; above, a score that is not zero is 2^23 at
+    // least, of sums of 2^-24 and up.)
+    r.cq[t] = fminf(fmaxf(a.scale2 * back, 0x1p-86f), 0x1p87f);
     r.limit[t] = !on || i >= nq ? 0 : a.causal ? max(len - nq + i + 1, 0) : len;
     r.m[t] = NONE;
     r.l[t] = 0.0f;
