@@ -83,6 +83,10 @@ __device__ __forceinline__ void load_block(Block& f, const uint8_t* kc, const ui
 // A block's magnitude as the sums take it.  A cleared buffer's, of a block that was never written, is zero: tokens of zeros, as
 // they are read back, and no quotient by it.
 __device__ __forceinline__ float held(float mag) { return fmaxf(mag, C8_LEAST); }
+// ... of the wave, as a scalar: magnitudes are not below zero, and compare as their bits do
+__device__ __forceinline__ uint32_t held_bits(float mag) {
+  return max((uint32_t)__builtin_amdgcn_readfirstlane(__float_as_uint(mag)), __float_as_uint(C8_LEAST));
+}
 
 // A row's maximum and denominator.  A query behind q_count went along where the others see every token: it has none, and
 // whatever it is (an infinity times a weight of none would be no number) it gives zeros.
@@ -484,7 +488,7 @@ __global__ __launch_bounds__(256, 2) void c8_many_kernel(C8Attn a, int tiles) {
     clear_dead(b0);
     put_v(b0, 0); put_v(b0, 1);
     put_k(b0 + 1, 0); put_k(b0 + 1, 1);
-    float kn = gkm, vn = gvm;              // of the next block
+    uint32_t kn = held_bits(gkm), vn = held_bits(gvm);          // of the next block
     gk = gk0;
     put_k(b0, 0); put_k(b0, 1);
     ask_k(b0 + 2);
@@ -500,7 +504,8 @@ __global__ __launch_bounds__(256, 2) void c8_many_kernel(C8Attn a, int tiles) {
       for (int k = 0; k < 8; ++k) weight(t, k);
       p[t] = pn[t];
     }
-    float rv = __builtin_amdgcn_rcpf(vm), vmost = vm;          // the largest magnitude so far
+    float rv = __builtin_amdgcn_rcpf(vm);
+    uint32_t vmost = held_bits(vm);        // the largest magnitude so far
     hand_over();
     // the weights of block i are there; block i + 1 is scored, and turned into weights between the products of block i
     for (int i = b0; i + 1 < b1; ++i) {
@@ -508,8 +513,9 @@ __global__ __launch_bounds__(256, 2) void c8_many_kernel(C8Attn a, int tiles) {
       // turns of a block each: 322 -> 311 us)
       if ((i ^ (blockIdx.x >> 8)) & 1) __builtin_amdgcn_s_setprio(1);
       else __builtin_amdgcn_s_setprio(0);
-      km = held(kn); vm = held(vn);
-      kn = gkm; vn = gvm;
+      km = __uint_as_float(kn); vm = __uint_as_float(vn);
+      const uint32_t vb = vn;
+      kn = held_bits(gkm); vn = held_bits(gvm);
       clear_dead(i + 1);
       scores(i + 1, [&](int g) {
         if (g < 2) put_k(i + 2, g);
@@ -522,8 +528,8 @@ __global__ __launch_bounds__(256, 2) void c8_many_kernel(C8Attn a, int tiles) {
       lv = __log2f(vm);
       const bool rise = maxima(i + 1, km, lv);
       factors(km, lv);
-      vmost = fmaxf(vmost, vm);
-      if (vm * FAR < vmost) {
+      vmost = max(vmost, vb);
+      if (vb + (3u << 23) < vmost) {
         far_sums(rv);
         rv = 0.0f;
       }
