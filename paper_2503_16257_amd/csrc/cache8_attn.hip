@@ -17,7 +17,7 @@ namespace vidkv {
 
 constexpr float RISE = 8.0f, UP = 7.0f;
 constexpr float NONE = -1e30f;             // a maximum of nothing
-constexpr float FAR = 8.0f;                // a block's values are far below another's: by more than this factor
+constexpr uint32_t FAR = 3u << 23;         // a block's values are far below another's: by more than 2^3 (exponents, in place)
 
 struct C8Attn {
   View q, out;
@@ -80,10 +80,8 @@ __device__ __forceinline__ void load_block(Block& f, const uint8_t* kc, const ui
   f.vm = vm[blk];
 }
 
-// A block's magnitude as the sums take it.  A cleared buffer's, of a block that was never written, is zero: tokens of zeros, as
-// they are read back, and no quotient by it.
-__device__ __forceinline__ float held(float mag) { return fmaxf(mag, C8_LEAST); }
-// ... of the wave, as a scalar: magnitudes are not below zero, and compare as their bits do
+// A block's magnitude as the sums take it, a wave's scalar.  A cleared buffer's, of a block that was never written, is zero: tokens
+// of zeros, as they are read back, and no quotient by it.  (Magnitudes are not below zero, and compare as their bits do.)
 __device__ __forceinline__ uint32_t held_bits(float mag) {
   return max((uint32_t)__builtin_amdgcn_readfirstlane(__float_as_uint(mag)), __float_as_uint(C8_LEAST));
 }
@@ -290,13 +288,14 @@ __global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : NT < 3 ? 2 : 1) void c8_few
   if (b0 < b1) load_block(f, a.kc, a.vc, a.km, a.vm, head + b0, lane);      // (on its way while the queries are laid out)
   load_rows<NT>(r, a, b, h, 0, rows, len, nq, lane);
   if (b0 < b1) {
-    float vmost = 0.0f;                    // the largest magnitude so far
+    uint32_t vmost = 0;                    // the largest magnitude so far
     for (int i = b0; i < b1; ++i) {
       if (i + 1 < b1) load_block(g, a.kc, a.vc, a.km, a.vm, head + i + 1, lane);
-      f.km = held(f.km);
-      f.vm = held(f.vm);
-      vmost = fmaxf(vmost, f.vm);
-      take_codes<NT, CODE>(r, f, (i + 1) * G > all, f.vm * FAR < vmost, i * G, len, lane);
+      const uint32_t kb = held_bits(f.km), vb = held_bits(f.vm);
+      f.km = __uint_as_float(kb);
+      f.vm = __uint_as_float(vb);
+      vmost = max(vmost, vb);
+      take_codes<NT, CODE>(r, f, (i + 1) * G > all, vb + FAR < vmost, i * G, len, lane);
       f = g;
     }
   }
@@ -399,7 +398,7 @@ __global__ __launch_bounds__(256, 2) void c8_many_kernel(C8Attn a, int tiles) {
   float km = 1.0f, vm = 1.0f;
   if (b0 < b1) {
     ask_k(b0);
-    gk0 = gk; km = held(gkm); vm = held(gvm);
+    gk0 = gk; km = gkm; vm = gvm;
     ask_v(b0);
     ask_k(b0 + 1);
   }
@@ -495,6 +494,8 @@ __global__ __launch_bounds__(256, 2) void c8_many_kernel(C8Attn a, int tiles) {
     ask_v(b0 + 1);
     hand_over();
     scores(b0, [](int) {});
+    km = __uint_as_float(held_bits(km));
+    vm = __uint_as_float(held_bits(vm));
     float lv = __log2f(vm);
     maxima(b0, km, lv);
     factors(km, lv);
@@ -505,7 +506,7 @@ __global__ __launch_bounds__(256, 2) void c8_many_kernel(C8Attn a, int tiles) {
       p[t] = pn[t];
     }
     float rv = __builtin_amdgcn_rcpf(vm);
-    uint32_t vmost = held_bits(vm);        // the largest magnitude so far
+    uint32_t vmost = __float_as_uint(vm);  // the largest magnitude so far
     hand_over();
     // the weights of block i are there; block i + 1 is scored, and turned into weights between the products of block i
     for (int i = b0; i + 1 < b1; ++i) {
@@ -529,7 +530,7 @@ __global__ __launch_bounds__(256, 2) void c8_many_kernel(C8Attn a, int tiles) {
       const bool rise = maxima(i + 1, km, lv);
       factors(km, lv);
       vmost = max(vmost, vb);
-      if (vb + (3u << 23) < vmost) {
+      if (vb + FAR < vmost) {
         far_sums(rv);
         rv = 0.0f;
       }
