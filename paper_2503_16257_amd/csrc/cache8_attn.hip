@@ -97,8 +97,8 @@ __device__ __forceinline__ f2 row_stats(const Rows<NT>& r, int t) {
 // takes them, rounded, so that equal ones are rounded alike above and below.  P carries A_v, the weight does not: where A_v is
 // far below the largest before it, P can lose bits in fp16, or vanish, whose weight is as large as any (a block of zeros has
 // A_v = 2^-40).  Such a block's sum is taken in float32; of others what fp16 loses is 2^-29 of the largest weight, a token.
-// (Many queries, vector units the bound: float32 for every second block 271 -> 306 us, for all of them 348; the look alone 3.
-// Few queries, memory the bound: the same times, 40 rows 25.5 -> 25.7 and 26.8.)
+// (196 queries over 98196 tokens, vector units the bound: no such block 271 us, every second one 302, all but the first 341; without
+// the look at the magnitudes 268.  Few queries, memory the bound: the same times, 40 rows 25.4, 26.7, 25.7.)
 __device__ __forceinline__ float sum_of(const Op& p) {
   Op ones;
 #pragma unroll
@@ -344,7 +344,7 @@ __global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : NT < 3 ? 2 : 1) void c8_few
 // reads a row - 48 rows are what 256 registers hold, two waves a SIMD (32 rows, three waves: 410 us where 48 took 352) -
 // the weights of a block are made between the products of the block before, the decoding between those of the scores, and
 // the denominators are products with ones.  196 queries x 28 heads over 98196 tokens, int8: 266 us, 1.04 PFLOP/s (1.16 with
-// the rows that pad the last tile); 6272 over themselves, causal: 274 us, 1.03.  On the way there: each wave decoding for
+// the rows that pad the last tile); 6272 over themselves, causal: 270 us, 1.04.  On the way there: each wave decoding for
 // itself from memory 902 and 750; the weights in a phase of their own 340 and 350; eight waves to a workgroup, half the
 // decoding each: the same.  32 x 32 x 16 products, which cost the vector units less, with 32 rows a wave: 460 and 355.
 // grid (tiles of rows x splits x B x H), heads fastest: the tiles that see most come first, and what shares a head's
