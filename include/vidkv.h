@@ -363,9 +363,10 @@ vidkv_status vidkv_rotary_apply(const vidkv_rotary *rot, int32_t inverse, int32_
  * it holds its magnitude A = max |x|, clamped to 2^-40..2^40, and codes
  *   code 0 (int8): rint(x * 127 / A), value = code * A / 127
  *   code 1 (e4m3): the nearest e4m3 number to x * 448 / A, value = that * A / 448
- * (ties to even in both).  An infinity is taken as its type's largest number, which
- * like any number far above the others leaves these few bits or none, tokens that
- * the block held before among them; a NaN is taken as zero. */
+ * (ties to even in both; |x| beyond A = 2^40 has the largest code).  An infinity is
+ * taken as its type's largest number, which like any number far above the others
+ * leaves these few bits or none, tokens that the block held before among them; a
+ * NaN is taken as zero. */
 typedef struct vidkv_cache8 {
   int32_t n_layers, batch, n_kv_heads;
   int32_t n_q_heads;      /* multiple of n_kv_heads, any ratio                   */

@@ -100,7 +100,8 @@ struct TF16 {
   }
   static __device__ __forceinline__ u32x4 pack8(f8v v) { return __builtin_bit_cast(u32x4, __builtin_convertvector(v, h8)); }
   static __device__ __forceinline__ float of_bits(uint32_t u) { return (float)__builtin_bit_cast(_Float16, (uint16_t)u); }
-  static constexpr uint16_t INF = 0x7c00, TOP = 0x7bff;        // bits of infinity, and of the largest magnitude that goes into a block: the type's
+  // bits of infinity, and of the largest magnitude that goes into a block: the type's
+  static constexpr uint16_t INF = 0x7c00, TOP = 0x7bff;
 };
 
 struct TBF16 {
@@ -129,7 +130,7 @@ struct TBF16 {
   }
   static __device__ __forceinline__ u32x4 pack8(f8v v) { return __builtin_bit_cast(u32x4, __builtin_convertvector(v, b8)); }
   static __device__ __forceinline__ float of_bits(uint32_t u) { return __uint_as_float(u << 16); }
-  static constexpr uint16_t INF = 0x7f80, TOP = 0x5380;        // ... C8_MOST
+  static constexpr uint16_t INF = 0x7f80, TOP = 0x5380;        // (C8_MOST)
 };
 
 struct TF32 {
