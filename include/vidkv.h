@@ -1,8 +1,9 @@
 /*
  * vidkv.h - C ABI of the MI355X (gfx950) VidKV hot path:
  *   sub-2-bit KV-cache codec + single-query GQA decode attention over the
- *   packed cache; beside it rotary positions on several axes and a cache in
- *   8 bits with its attention (second half of this file).
+ *   packed cache; beside it rotary positions on several axes, a cache in
+ *   8 bits with its attention, and trees of drafted tokens checked against it
+ *   (second half of this file).
  *
  * Method (arXiv 2503.16257): keys are quantized per channel with mixed
  * precision - the n_anom channels of largest range get the 2-bit uniform
@@ -443,6 +444,112 @@ vidkv_status vidkv_cache8_attention(const vidkv_cache8 *p, int32_t layer, int32_
                                     const int32_t *q_count_dev, const vidkv_view *out,
                                     void *workspace_dev, size_t workspace_bytes,
                                     void *hip_stream);
+
+/* ---- trees of drafted tokens --------------------------------------------------
+ * Checking several drafted tokens in one step of the target model.  Node 0 of a
+ * sequence's tree is the last token that was sampled, whose successor is asked for;
+ * node i > 0 is a drafted token behind node parent[i] < i.  The nodes' keys and
+ * values stay in 16 bits beside the 8-bit cache - a token that is turned down would
+ * leave its magnitude in a block's codes - and those that stand are appended to it:
+ *   once a step       vidkv_tree_masks: what each node sees, and its position
+ *   in every layer    vidkv_rotary_apply, vidkv_cache8_tree_attention
+ *   once a step       vidkv_tree_verify, vidkv_cache8_append_path (all layers)
+ * A tree has 1..VIDKV_TREE_NODES nodes; count_dev[b] (taken as 0..n_nodes, NULL:
+ * n_nodes) says how many of them sequence b has.                                */
+#define VIDKV_TREE_NODES 256
+#define VIDKV_TREE_VOCAB (1 << 22)
+
+/* Masks and positions.  A node sees itself and its ancestors.
+ *   parent_dev in : [B, n_nodes] int32; -1 or anything else outside 0..i-1: node i
+ *                   has no ancestors.  NULL: a chain, node i is behind node i - 1
+ *   mask_dev  out : [B, n_nodes, ceil(n_nodes / 64)] uint64: bit j % 64 of word
+ *                   j / 64 of node i: it sees node j.  None for nodes from count on
+ *   pos_dev   out : [n_axes, B, n_nodes] int32 as vidkv_rotary_apply takes them,
+ *                   n_axes 1..4: base_dev[b] and the node's ancestors in number on
+ *                   every axis (base from count on); both NULL: none             */
+vidkv_status vidkv_tree_masks(int32_t batch, int32_t n_nodes, const int32_t *parent_dev,
+                              const int32_t *count_dev, uint64_t *mask_dev, int32_t n_axes,
+                              const int32_t *base_dev, int32_t *pos_dev, void *hip_stream);
+
+/* out_i = Softmax(scale * q_i [K'; K]^T) [V'; V]: the first length[b] tokens of one
+ * layer of the cache, and the nodes that mask i has, of count[b] there are (any mask: its bits
+ * from count on are not looked at).  A node without any and the rows from count[b]
+ * on get zeros.  K and V are taken as the cache takes them where they leave its range
+ * (an infinity as its type's largest number, a NaN as zero, bf16 held to 2^40),
+ * else as they are; their rows from count[b] on are not read.  Precision as
+ * vidkv_cache8_attention.
+ *   q, out, K, V   : [B, Hq, n_nodes, 128] and [B, Hkv, n_nodes, 128], all fp16 or
+ *                    all bf16
+ *   mask_dev    in : [B, n_nodes, ceil(n_nodes / 64)] uint64, 8-byte aligned
+ *   workspace_dev  : >= vidkv_cache8_workspace_bytes(p, n_nodes) bytes            */
+vidkv_status vidkv_cache8_tree_attention(const vidkv_cache8 *p, int32_t layer, int32_t n_nodes,
+                                         const vidkv_view *q, const vidkv_view *K,
+                                         const vidkv_view *V, const uint64_t *mask_dev,
+                                         const void *cache_dev, size_t cache_bytes,
+                                         const int32_t *length_dev, const int32_t *count_dev,
+                                         const vidkv_view *out, void *workspace_dev,
+                                         size_t workspace_bytes, void *hip_stream);
+
+/* Rows of probabilities, [B, n_nodes, vocab]: a row's entries lie next to each other, rows
+ * wherever their elements are aligned. */
+typedef struct vidkv_rows {
+  const void *data;       /* device */
+  int64_t stride_batch;   /* in elements */
+  int64_t stride_row;
+  int32_t dtype;          /* vidkv_dtype, fp32, fp16 or bf16 */
+} vidkv_rows;
+
+/* Which drafted tokens stand, and the token behind them, so that what comes out is
+ * distributed as if it were sampled from the target model token by token.  From node 0
+ * on, the children of the node reached are tried in order; R is what is left of target
+ * row u of that node, taken to sum to one.
+ *   draft NULL        the drafted tokens are no random ones.  Token x of child i
+ *                     stands if uniform[i] < R(x); else R(x) becomes 0
+ *   draft, distinct 0 each child was drawn from row u of draft, Q: x stands if
+ *                     uniform[i] Q(x) < R(x); else R becomes max(R - Q, 0)
+ *   draft, distinct 1 children were drawn without putting back: likewise, and Q(x)
+ *                     becomes 0 and Q is divided by what is left of it
+ * and R is divided by its sum.  The walk goes on at a child that stands, with its rows, and ends where no
+ * child does.  The next token is the first v with sum_{w <= v} R(w) > uniform[0] sum R (the
+ * last with R(v) > 0 if there is none).  Without draft, and with distinct, a token that an earlier
+ * sibling had is passed over, as is one outside 0..vocab-1.  Where nothing at
+ * all would be left of R (with numbers in [0, 1): by rounding alone), with draft it stays what it was and no
+ * further child is tried, without it is the target's row again.
+ * Sums and decisions are in 64 bits.  Entries have to be finite; those not above 0 count as 0.
+ *   target     in : probabilities behind each node.  draft: of target's dtype
+ *   token_dev  in : [B, n_nodes] int32 (node 0's is not looked at)
+ *   parent_dev in : [B, n_nodes] int32; outside 0..i-1: node i is no child.  NULL: a chain
+ *   uniform_dev in: [B, n_nodes] float32, independent numbers in [0, 1)
+ *   path_dev  out : [B, n_nodes] int32: node 0 and the nodes that stand, then -1
+ *   accepted_dev out: [B] int32: the nodes of the path, 1 at least (0 where count[b] is 0)
+ *   next_dev  out : [B] int32: the next token; -1 where count[b] is 0 or the last node's row has nothing
+ *                   above 0
+ *   workspace_dev : >= vidkv_tree_verify_workspace_bytes(..) bytes, 256-byte aligned
+ * The size query gives 0 for sizes outside 1..65535, 1..VIDKV_TREE_NODES and
+ * 1..VIDKV_TREE_VOCAB (the call: VIDKV_ESHAPE). */
+size_t vidkv_tree_verify_workspace_bytes(int32_t batch, int32_t n_nodes, int32_t vocab);
+vidkv_status vidkv_tree_verify(int32_t batch, int32_t n_nodes, int32_t vocab,
+                               const vidkv_rows *target, const vidkv_rows *draft, int32_t distinct,
+                               const int32_t *token_dev, const int32_t *parent_dev,
+                               const int32_t *count_dev, const float *uniform_dev,
+                               int32_t *path_dev, int32_t *accepted_dev, int32_t *next_dev,
+                               void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+
+/* Appends nodes path[b][0 .. accepted[b] - 1] of all layers as tokens start[b],
+ * start[b] + 1, ..., the same as vidkv_cache8_write of those rows in every layer
+ * would.  K and V are those of layer 0; layer l's are l * k_stride_layer (V: v_stride_layer)
+ * elements further on.
+ *   K, V        in : [B, Hkv, n_nodes, 128], fp16 or bf16, both the same dtype, turned already
+ *   path_dev    in : [B, n_nodes] int32, as vidkv_tree_verify leaves it: any nodes
+ *                    in any order; the path ends before an entry outside 0..n_nodes-1
+ *   accepted_dev in: [B] int32 (taken as 0..n_nodes)
+ *   start_dev   in : [B] int32; negative: nothing is written; tokens behind the capacity
+ *                    are dropped                                                   */
+vidkv_status vidkv_cache8_append_path(const vidkv_cache8 *p, int32_t n_nodes, const vidkv_view *K,
+                                      int64_t k_stride_layer, const vidkv_view *V,
+                                      int64_t v_stride_layer, const int32_t *path_dev,
+                                      const int32_t *accepted_dev, const int32_t *start_dev,
+                                      void *cache_dev, size_t cache_bytes, void *hip_stream);
 
 /* Measurement aids, not part of the method.  Each takes the arguments of the
  * entry point it is named after, checks them the same way, and launches only

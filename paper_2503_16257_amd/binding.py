@@ -57,6 +57,13 @@ class VidkvCache8(C.Structure):
                 ("head_dim", C.c_int32), ("capacity", C.c_int32), ("code", C.c_int32), ("softmax_scale", C.c_float)]
 
 
+class VidkvRows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride_batch", C.c_int64), ("stride_row", C.c_int64), ("dtype", C.c_int32)]
+
+
+TREE_NODES, TREE_VOCAB = 256, 1 << 22    # VIDKV_TREE_NODES, VIDKV_TREE_VOCAB
+
+
 class VidkvSideStream(C.Structure):
     _fields_ = [("hip_stream", C.c_void_p), ("fork_event", C.c_void_p), ("join_event", C.c_void_p)]
 
@@ -154,6 +161,17 @@ def lib() -> C.CDLL:
         L.vidkv_cache8_read.restype = C.c_int
         L.vidkv_cache8_attention.argtypes = [CP, i32, i32, i32, VP, vp, sz, vp, vp, VP, vp, sz, vp]
         L.vidkv_cache8_attention.restype = C.c_int
+        WP, i64 = C.POINTER(VidkvRows), C.c_int64
+        L.vidkv_tree_masks.argtypes = [i32, i32, vp, vp, vp, i32, vp, vp, vp]
+        L.vidkv_tree_masks.restype = C.c_int
+        L.vidkv_cache8_tree_attention.argtypes = [CP, i32, i32, VP, VP, VP, vp, vp, sz, vp, vp, VP, vp, sz, vp]
+        L.vidkv_cache8_tree_attention.restype = C.c_int
+        L.vidkv_tree_verify_workspace_bytes.argtypes = [i32, i32, i32]
+        L.vidkv_tree_verify_workspace_bytes.restype = sz
+        L.vidkv_tree_verify.argtypes = [i32, i32, i32, WP, WP, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.vidkv_tree_verify.restype = C.c_int
+        L.vidkv_cache8_append_path.argtypes = [CP, i32, VP, i64, VP, i64, vp, vp, vp, vp, sz, vp]
+        L.vidkv_cache8_append_path.restype = C.c_int
         L.vidkv_status_string.argtypes = [C.c_int]
         L.vidkv_status_string.restype = C.c_char_p
         L.vidkv_abi_version.argtypes = []
@@ -224,13 +242,13 @@ def workspace_bytes(p: VidkvParams, which: int) -> int:
 # plain (host time with and without, in turn in one process: 6.9 against 9.0 us a decode call, 3.5 against 5.7 a flush, in
 # another 7.8 against 10.0 and 4.2 against 5.8; the launches are 3 us each), and what follows is kept to a few
 # attribute reads per tensor.  torch's names are looked up once, with the library.
-_Tensor = _f16 = _u8 = _f32 = _i32 = _raw_stream = _cur_device = None
+_Tensor = _f16 = _u8 = _f32 = _i32 = _i64 = _raw_stream = _cur_device = None
 _dtypes = {}             # of views: torch's to vidkv_dtype
 
 
 def _bind_torch(torch) -> None:
-    global _Tensor, _f16, _u8, _f32, _i32, _raw_stream, _cur_device
-    _f16, _u8, _f32, _i32 = torch.float16, torch.uint8, torch.float32, torch.int32
+    global _Tensor, _f16, _u8, _f32, _i32, _i64, _raw_stream, _cur_device
+    _f16, _u8, _f32, _i32, _i64 = torch.float16, torch.uint8, torch.float32, torch.int32, torch.int64
     _dtypes.update({torch.float16: 0, torch.bfloat16: 1, torch.float32: 2})
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     _cur_device = torch.cuda.current_device
@@ -544,6 +562,106 @@ def cache8_attention(p: VidkvCache8, layer: int, cache, q, out, length, workspac
         return
     _check(L.vidkv_cache8_attention(C.byref(p), layer, n, int(causal), _ref(vq), *a, _stream(stream)),
            "vidkv_cache8_attention")
+
+
+# ---- trees of drafted tokens: node 0 is the last token that was sampled, node i > 0 is drafted behind parents[b][i] < i ----
+
+def _nodes(t, name):
+    """Batch and nodes of an int32 [B, n] tensor."""
+    if not isinstance(t, _Tensor) or t.dim() != 2:
+        raise ValueError(f"{name}: expected a tensor [batch, nodes]")
+    return t.shape[0], t.shape[1]
+
+
+def tree_masks(parents, masks, base=None, positions=None, count=None, stream=None) -> None:
+    """vidkv_tree_masks: parents [B,n] int32 -> masks [B,n,ceil(n/64)] int64, the nodes that each node sees as bits, and, with
+    base [B] int32, positions [n_axes,B,n] int32.  parents None: chains, of the masks' sizes.  count[b]: nodes that there are
+    (None: all n)."""
+    L = _lib or lib()
+    if not isinstance(masks, _Tensor) or masks.dim() != 3:
+        raise ValueError("masks: expected a tensor [batch, nodes, words]")
+    B, n = masks.shape[0], masks.shape[1]
+    if (base is None) != (positions is None):
+        raise ValueError("tree_masks: base and positions come together")
+    axes = 0
+    if positions is not None:
+        axes = positions.shape[0] if isinstance(positions, _Tensor) and positions.dim() == 3 else -1
+    _check(L.vidkv_tree_masks(B, n, _arg(parents, _i32, "parents", (B, n)), _arg(count, _i32, "count", (B,)),
+                              _arg(masks, _i64, "masks", (B, n, (n + 63) // 64)), axes, _arg(base, _i32, "base", (B,)),
+                              _arg(positions, _i32, "positions", (axes, B, n)), _stream(stream)), "vidkv_tree_masks")
+
+
+def cache8_tree_attention(p: VidkvCache8, layer: int, cache, q, K, V, masks, out, length, workspace, count=None,
+                          stream=None) -> None:
+    """vidkv_cache8_tree_attention: the nodes' queries q [B,Hq,n,128] over the first length[b] tokens of the cache and the
+    nodes of K, V [B,Hkv,n,128] that masks [B,n,words] int64 has for each -> out.  The workspace is that of
+    cache8_attention (cache8_workspace_bytes(p, n))."""
+    L = _lib or lib()
+    n = q.shape[2] if isinstance(q, _Tensor) and q.dim() == 4 else -1
+    shape, kv = (p.batch, p.n_q_heads, n, 128), (p.batch, p.n_kv_heads, n, 128)
+    vq, vk, vv, vo = _view(q, "q", shape), _view(K, "K", kv), _view(V, "V", kv), _view(out, "out", shape, True)
+    _check(L.vidkv_cache8_tree_attention(
+        C.byref(p), layer, n, _ref(vq), _ref(vk), _ref(vv), _arg(masks, _i64, "masks", (p.batch, n, (n + 63) // 64)),
+        _arg(cache, _u8, "cache"), _nbytes(cache), _arg(length, _i32, "length", (p.batch,)),
+        _arg(count, _i32, "count", (p.batch,)), _ref(vo), _arg(workspace, _u8, "workspace"), _nbytes(workspace),
+        _stream(stream)), "vidkv_cache8_tree_attention")
+
+
+def tree_verify_workspace_bytes(batch: int, n_nodes: int, vocab: int) -> int:
+    return lib().vidkv_tree_verify_workspace_bytes(batch, n_nodes, vocab)
+
+
+def _rows(t, name, shape):
+    """Rows of probabilities [B, n, vocab] of any strides, entries next to each other, as a VidkvRows (None -> NULL)."""
+    if t is None:
+        return None
+    if not isinstance(t, _Tensor) or not t.is_cuda:
+        raise TypeError(f"{name}: expected a CUDA tensor")
+    _here(t, name)
+    code = _dtypes.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name}: expected float16, bfloat16 or float32, got {t.dtype}")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
+    b, r, c = t.stride()
+    if c != 1 and shape[2] > 1:
+        raise ValueError(f"{name}: the entries of a row must lie next to each other")
+    return VidkvRows(t.data_ptr(), b if shape[0] > 1 else 0, r if shape[1] > 1 else 0, code)
+
+
+def tree_verify(target, tokens, uniform, path, accepted, next_token, workspace, draft=None, parents=None, count=None,
+                distinct: bool = False, stream=None) -> None:
+    """vidkv_tree_verify: target [B,n,vocab] probabilities (float32, float16, bfloat16) behind each node, tokens [B,n] int32,
+    uniform [B,n] float32 in [0, 1) -> path [B,n] (nodes that stand, then -1), accepted [B] (how many), next_token [B], all int32.
+    draft [B,n,vocab]: what the children of each node were drawn from, with `distinct` without putting back; None: they are no
+    random ones.  parents None: chains."""
+    L = _lib or lib()
+    B, n = _nodes(tokens, "tokens")
+    V = target.shape[2] if isinstance(target, _Tensor) and target.dim() == 3 else -1
+    t, d = _rows(target, "target", (B, n, V)), _rows(draft, "draft", (B, n, V))
+    a = [_arg(tokens, _i32, "tokens", (B, n)), _arg(parents, _i32, "parents", (B, n)), _arg(count, _i32, "count", (B,)),
+         _arg(uniform, _f32, "uniform", (B, n)), _arg(path, _i32, "path", (B, n)), _arg(accepted, _i32, "accepted", (B,)),
+         _arg(next_token, _i32, "next_token", (B,)), _arg(workspace, _u8, "workspace"), _nbytes(workspace)]
+    if B == 0:
+        return
+    _check(L.vidkv_tree_verify(B, n, V, _ref(t), _ref(d), int(distinct), *a, _stream(stream)), "vidkv_tree_verify")
+
+
+def cache8_append_path(p: VidkvCache8, cache, K, V, path, accepted, start, stream=None) -> None:
+    """vidkv_cache8_append_path: of K, V [n_layers,B,Hkv,n,128] fp16 / bf16 the nodes path[b][:accepted[b]] coded as tokens
+    start[b].. of every layer."""
+    L = _lib or lib()
+    B, n = _nodes(path, "path")
+    v, layer = [], []
+    for t, name in ((K, "K"), (V, "V")):
+        if not isinstance(t, _Tensor) or t.dim() != 5 or t.shape[0] != p.n_layers:
+            raise ValueError(f"{name}: expected a tensor [{p.n_layers}, batch, heads, nodes, 128]")
+        v.append(_view(t[0], name, (p.batch, p.n_kv_heads, n, 128)))
+        layer.append(t.stride(0) if p.n_layers > 1 else 0)
+    _check(L.vidkv_cache8_append_path(
+        C.byref(p), n, _ref(v[0]), layer[0], _ref(v[1]), layer[1], _arg(path, _i32, "path", (p.batch, n)),
+        _arg(accepted, _i32, "accepted", (p.batch,)), _arg(start, _i32, "start", (p.batch,)), _arg(cache, _u8, "cache"),
+        _nbytes(cache), _stream(stream)), "vidkv_cache8_append_path")
 
 
 def calib_copy(dst, src, stream=None) -> None:

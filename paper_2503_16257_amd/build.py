@@ -17,7 +17,7 @@ MARSHAL = os.path.join(HERE, "vidkv_marshal.so")
 SOURCES = ["vidkv_api.hip", "quant_keys.hip", "quant_keys_mfma.hip", "quant_values.hip",
            "quant_values_enc.hip", "decode_attn.hip", "decode_attn_mfma.hip", "decode_attn_mfma_b.hip",
            "decode_attn_mfma_c.hip", "decode_attn_mfma_t.hip", "saliency.hip", "rotary.hip", "cache8.hip",
-           "cache8_attn.hip", "cache8_api.hip"]
+           "cache8_attn.hip", "cache8_tree.hip", "cache8_append.hip", "tree.hip", "cache8_api.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     # packed-fp32 VALU forms are kept off for all device code

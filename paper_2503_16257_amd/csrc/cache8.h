@@ -201,6 +201,17 @@ __device__ __forceinline__ void turn_runs(V& x, V& y, bool adjacent, const float
   }
 }
 
+typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+
+// Two elements held to the largest magnitude that goes into a block: an infinity is the type's largest number, a NaN a zero,
+// so that no code is one (a weight of zero times it would be a NaN in rows that do not see its token).
+template <class T>
+__device__ __forceinline__ uint32_t held(uint32_t u) {
+  const uint32_t a = u & 0x7fffu, b = u >> 16 & 0x7fffu, lo = a > T::INF ? 0 : min(a, (uint32_t)T::TOP),
+                 hi = b > T::INF ? 0 : min(b, (uint32_t)T::TOP);
+  return (u & 0x80008000u) | lo | hi << 16;
+}
+
 // ---- codes ----------------------------------------------------------------------------------
 template <int CODE> constexpr float kLevel = CODE == 0 ? 127.0f : 448.0f;
 

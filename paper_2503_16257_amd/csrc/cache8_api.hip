@@ -1,7 +1,8 @@
-// C ABI of the rotary positions and the 8-bit cache: argument checks on the host, then launches on the caller's stream.
+// C ABI of the rotary positions, the 8-bit cache and the trees of drafted tokens: argument checks on the host, then launches on the caller's stream.
 #include <cmath>
 
 #include "cache8.h"
+#include "tree.h"
 
 namespace vidkv {
 hipError_t launch_rotary(const vidkv_rotary* r, int inverse, int B, int n, const int32_t* pos, int Hq, const vidkv_view* q,
@@ -42,6 +43,21 @@ bool good_rotary(const vidkv_rotary* r) {
   for (int i = 0; i < r->rot_dim / 2; ++i)
     if (r->axis[i] >= r->n_axes) return false;
   return true;
+}
+
+bool good_nodes(int32_t n) { return n >= 1 && n <= VIDKV_TREE_NODES; }
+
+// Rows of probabilities that a kernel can take: elements where they are aligned.
+bool good_rows(const vidkv_rows* r) {
+  if (!r || !r->data || (r->dtype != VIDKV_F16 && r->dtype != VIDKV_BF16 && r->dtype != VIDKV_F32)) return false;
+  const int64_t most = (int64_t)1 << 48;
+  for (int64_t s : {r->stride_batch, r->stride_row})
+    if (s < -most || s > most) return false;
+  return at(r->data, dtype_bytes(r->dtype));
+}
+Probs make_probs(const vidkv_rows* r) {
+  const long long e = r ? dtype_bytes(r->dtype) : 0;
+  return r ? Probs{static_cast<const char*>(r->data), r->stride_batch * e, r->stride_row * e} : Probs{};
 }
 
 // Tokens of a call, and rows (queries x heads of a group): HIP counts a grid dimension's threads in 32 bits.
@@ -166,6 +182,81 @@ vidkv_status vidkv_cache8_attention(const vidkv_cache8* p, int32_t layer, int32_
   if (!stream_on_current_device(static_cast<hipStream_t>(stream))) return VIDKV_EINVAL;
   const hipError_t e = launch_c8_attn(g, layer, n_query, causal, p->softmax_scale, q, static_cast<const uint8_t*>(cache),
                                       length, q_count, out, ws, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? VIDKV_OK : VIDKV_EHIP;
+}
+
+vidkv_status vidkv_tree_masks(int32_t batch, int32_t n_nodes, const int32_t* parent, const int32_t* count, uint64_t* mask,
+                              int32_t n_axes, const int32_t* base, int32_t* pos, void* stream) {
+  if (!mask || (base != nullptr) != (pos != nullptr)) return VIDKV_EINVAL;
+  if (batch < 0 || batch > 65535 || !good_nodes(n_nodes)) return VIDKV_ESHAPE;
+  if (pos && (n_axes < 1 || n_axes > 4)) return VIDKV_EINVAL;
+  if (!at(parent, 4) || !at(count, 4) || !at(base, 4) || !at(pos, 4) || !at(mask, 8)) return VIDKV_EINVAL;
+  if (!stream_on_current_device(static_cast<hipStream_t>(stream))) return VIDKV_EINVAL;
+  if (batch == 0) return VIDKV_OK;
+  const TreeMasks a{parent, count, base, mask, pos, n_nodes, n_axes};
+  return launch_tree_masks(a, batch, static_cast<hipStream_t>(stream)) == hipSuccess ? VIDKV_OK : VIDKV_EHIP;
+}
+
+vidkv_status vidkv_cache8_tree_attention(const vidkv_cache8* p, int32_t layer, int32_t n_nodes, const vidkv_view* q,
+                                         const vidkv_view* K, const vidkv_view* V, const uint64_t* mask, const void* cache,
+                                         size_t cache_bytes, const int32_t* length, const int32_t* count, const vidkv_view* out,
+                                         void* ws, size_t ws_bytes, void* stream) {
+  C8Geom g;
+  if (!p || !cache || !length || !ws || !mask) return VIDKV_EINVAL;
+  if (!make_c8(p, &g) || !good_nodes(n_nodes)) return VIDKV_ESHAPE;
+  if (layer < 0 || layer >= g.L) return VIDKV_EINVAL;
+  if (!(p->softmax_scale > 0.0f) || !(p->softmax_scale < 1e30f)) return VIDKV_EINVAL;
+  if (!few_enough(g, n_nodes) || !c8_attn_fits(g, n_nodes)) return VIDKV_ESHAPE;
+  for (const vidkv_view* v : {q, K, V, out})
+    if (!good_view(v, false) || v->dtype != q->dtype) return VIDKV_EINVAL;
+  if (!at(cache, 256) || !at(ws, 256) || !at(length, 4) || !at(count, 4) || !at(mask, 8)) return VIDKV_EINVAL;
+  if (cache_bytes < g.total || ws_bytes < c8_attn_ws_need(g, n_nodes)) return VIDKV_ENOSPACE;
+  if (!stream_on_current_device(static_cast<hipStream_t>(stream))) return VIDKV_EINVAL;
+  const hipError_t e = launch_c8_tree(g, layer, n_nodes, p->softmax_scale, q, K, V, mask, static_cast<const uint8_t*>(cache), length,
+                                      count, out, ws, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? VIDKV_OK : VIDKV_EHIP;
+}
+
+size_t vidkv_tree_verify_workspace_bytes(int32_t batch, int32_t n_nodes, int32_t vocab) {
+  if (batch < 1 || batch > 65535 || !good_nodes(n_nodes) || vocab < 1 || vocab > VIDKV_TREE_VOCAB) return 0;
+  return tree_verify_ws_bytes(batch, n_nodes, vocab);
+}
+
+vidkv_status vidkv_tree_verify(int32_t batch, int32_t n_nodes, int32_t vocab, const vidkv_rows* target, const vidkv_rows* draft,
+                               int32_t distinct, const int32_t* token, const int32_t* parent, const int32_t* count,
+                               const float* uniform, int32_t* path, int32_t* accepted, int32_t* next, void* ws, size_t ws_bytes,
+                               void* stream) {
+  if (!token || !uniform || !path || !accepted || !next || !ws) return VIDKV_EINVAL;
+  if (batch < 0 || batch > 65535 || !good_nodes(n_nodes) || vocab < 1 || vocab > VIDKV_TREE_VOCAB) return VIDKV_ESHAPE;
+  if ((distinct != 0 && distinct != 1) || (distinct && !draft)) return VIDKV_EINVAL;
+  if (!good_rows(target) || (draft && (!good_rows(draft) || draft->dtype != target->dtype))) return VIDKV_EINVAL;
+  for (const void* v : {(const void*)token, (const void*)parent, (const void*)count, (const void*)uniform, (const void*)path,
+                        (const void*)accepted, (const void*)next})
+    if (!at(v, 4)) return VIDKV_EINVAL;
+  if (!at(ws, 256)) return VIDKV_EINVAL;
+  if (!stream_on_current_device(static_cast<hipStream_t>(stream))) return VIDKV_EINVAL;
+  if (batch == 0) return VIDKV_OK;
+  if (ws_bytes < tree_verify_ws_bytes(batch, n_nodes, vocab)) return VIDKV_ENOSPACE;
+  const TreeVerify a{make_probs(target), make_probs(draft), token, parent, count, uniform, path, accepted, next,
+                     n_nodes, vocab, distinct};
+  return launch_tree_verify(a, target->dtype, batch, ws, static_cast<hipStream_t>(stream)) == hipSuccess ? VIDKV_OK : VIDKV_EHIP;
+}
+
+vidkv_status vidkv_cache8_append_path(const vidkv_cache8* p, int32_t n_nodes, const vidkv_view* K, int64_t k_stride_layer,
+                                      const vidkv_view* V, int64_t v_stride_layer, const int32_t* path, const int32_t* accepted,
+                                      const int32_t* start, void* cache, size_t cache_bytes, void* stream) {
+  C8Geom g;
+  if (!p || !cache || !path || !accepted || !start) return VIDKV_EINVAL;
+  if (!make_c8(p, &g) || !good_nodes(n_nodes) || !c8_append_fits(g, n_nodes)) return VIDKV_ESHAPE;
+  if (!good_view(K, false) || !good_view(V, false) || K->dtype != V->dtype) return VIDKV_EINVAL;
+  const int64_t most = (int64_t)1 << 48;
+  for (int64_t s : {k_stride_layer, v_stride_layer})
+    if (s % 8 || s < -most || s > most) return VIDKV_EINVAL;
+  if (!at(cache, 256) || !at(path, 4) || !at(accepted, 4) || !at(start, 4)) return VIDKV_EINVAL;
+  if (cache_bytes < g.total) return VIDKV_ENOSPACE;
+  if (!stream_on_current_device(static_cast<hipStream_t>(stream))) return VIDKV_EINVAL;
+  const hipError_t e = launch_c8_append(g, n_nodes, K, k_stride_layer, V, v_stride_layer, path, accepted, start,
+                                        static_cast<uint8_t*>(cache), static_cast<hipStream_t>(stream));
   return e == hipSuccess ? VIDKV_OK : VIDKV_EHIP;
 }
 
