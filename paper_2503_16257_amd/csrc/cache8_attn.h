@@ -272,6 +272,8 @@ __device__ __forceinline__ void put_out(const C8Attn& a, int b, int h, int row, 
 // ---- drafted tokens ---------------------------------------------------------------------------
 // Behind the cached tokens a row can see drafted ones, whose keys and values are given beside the cache in 16 bits: blocks
 // of 32 of them, of the magnitude `level`, so that their elements are in the codes' units as they are.
+static_assert(sizeof(C8Attn) % 8 == 0 && alignof(C8Attn) == 8, "Tree::argument()");
+
 struct NoTree {
   static constexpr bool ON = false;
 };
@@ -279,6 +281,14 @@ template <class T>
 struct Tree {
   static constexpr bool ON = true;
   typedef T Type;
+  // A kernel's second argument, read where it is asked for: held over the cached tokens it costs the scalar registers that their
+  // loop goes by (48 rows, 16 sequences of up to 6001 tokens: 29.4 us, 35 registers spilled).  Arguments lie behind each other.
+  static __device__ __forceinline__ Tree argument() {
+    typedef const __attribute__((address_space(4))) char* Args;
+    Args p = (Args)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const Tree*)(const char*)(p + sizeof(C8Attn));
+  }
   View K, V;                   // [B][H][n][128]
   const uint32_t* mask;        // [B][n][words]: bit j % 32 of word j / 32: the node sees node j
   int words;
@@ -417,62 +427,65 @@ __device__ __forceinline__ void take_tree(Rows<NT>& r, const K& k, const V& v, c
   }
 }
 
-// One such block by a wave for itself; its values go through 8 KB of LDS, `ops`, of its own.  TIGHT: keys are asked for when the
-// values' registers are free again.
-template <class T, int CODE, bool TIGHT, int NT>
-__device__ __forceinline__ void take_tree_alone(Rows<NT>& r, const Tree<T>& tree, const C8Attn& a, int b, int h, int rows, int nq, int blk,
-                                                bool far, u32x4* ops, int lane) {
-  const int x = lane & 15, kb = lane >> 4, t0 = blk * G;
-  const char* K = tree.K.data + b * tree.K.sb + h * tree.K.sh;
-  const char* V = tree.V.data + b * tree.V.sb + h * tree.V.sh;
-  Op k[2][4];
+// One such block by a wave for itself: operands through LDS, 8 KB each of its own (keys [8][64], values [8][64]).  TIGHT: keys are asked
+// for when the values' registers are free again.
+template <class T, bool TIGHT, int NT>
+struct TreeBlock {
+  u32x4 k[8];
   uint32_t v[4][8], sees[NT];
-  auto ask_k = [&] {
+  const char* K;
+  long long k_stride;
+  int blk, nq;
+
+  __device__ __forceinline__ void ask_keys(int lane) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) k[i >> 2][i & 3].q = tree_key<T>(K, tree.K.st, t0 + 16 * (i >> 2) + x, i & 3, nq, kb);
+    for (int i = 0; i < 8; ++i) k[i] = tree_key<T>(K, k_stride, blk * G + 16 * (i >> 2) + (lane & 15), i & 3, nq, lane >> 4);
+  }
+  __device__ __forceinline__ void ask(const C8Attn& a, int b, int h, int rows, int nodes, int block, int lane) {
+    const Tree<T> tree = Tree<T>::argument();
+    blk = block;
+    nq = nodes;
+    asm volatile("" : "+s"(b), "+s"(h));                 // (addresses are made again at every block: not kept over the cached tokens)
+    K = tree.K.data + b * tree.K.sb + h * tree.K.sh;
+    k_stride = tree.K.st;
+    const char* V = tree.V.data + b * tree.V.sb + h * tree.V.sh;
     load_sees(sees, tree, a, b, 0, rows, nq, blk, lane);
-  };
-  if (!TIGHT) ask_k();
+    if (!TIGHT) ask_keys(lane);
 #pragma unroll
-  for (int g = 0; g < 4; ++g) tree_values<T>(v[g], V, tree.V.st, t0, g, nq, lane);
-  us2 m{0, 0};
-#pragma unroll
-  for (int g = 0; g < 4; ++g) m = most_of<T>(m, v[g]);
-  if (beyond<T>(m)) {
-#pragma unroll
-    for (int i = 0; i < 32; ++i) v[i >> 3][i & 7] = held<T>(v[i >> 3][i & 7]);
+    for (int g = 0; g < 4; ++g) tree_values<T>(v[g], V, tree.V.st, blk * G, g, nq, lane);
   }
+  __device__ __forceinline__ void put(u32x4* keys, u32x4* values, int lane) {
+    us2 m{0, 0};
 #pragma unroll
-  for (int g = 0; g < 4; ++g) put_values(ops, v[g], g, lane);
-  if (TIGHT) {
-    hold_order();
-    ask_k();
+    for (int g = 0; g < 4; ++g) m = most_of<T>(m, v[g]);
+    if (beyond<T>(m)) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) v[i >> 3][i & 7] = held<T>(v[i >> 3][i & 7]);
+    }
+#pragma unroll
+    for (int g = 0; g < 4; ++g) put_values(values, v[g], g, lane);
+    if (TIGHT) {
+      hold_order();
+      ask_keys(lane);
+    }
+    m = us2{0, 0};
+#pragma unroll
+    for (int i = 0; i < 32; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(us2, k[i >> 2][i & 3] & 0x7fff7fffu));
+    if (beyond<T>(m)) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) k[i >> 2][i & 3] = held<T>(k[i >> 2][i & 3]);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) keys[i * 64 + lane] = k[i];
   }
-  m = us2{0, 0};
-#pragma unroll
-  for (int i = 0; i < 8; ++i) m = most_of<T>(m, k[i >> 2][i & 3].u);
-  if (beyond<T>(m)) {
-#pragma unroll
-    for (int i = 0; i < 32; ++i) k[i >> 4][i >> 2 & 3].u[i & 3] = held<T>(k[i >> 4][i >> 2 & 3].u[i & 3]);
-  }
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  take_tree<T, CODE>(
-      r, [&](int tt, int j) { return k[tt][j]; },
-      [&](int c) {
-        Op o;
-        o.q = ops[c * 64 + lane];
-        return o;
-      },
-      sees, far, lane);
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-}
+};
 
 // W waves share out the blocks of a split, for up to 16 NT rows a KV head.  Bound by HBM, 256 bytes a token and KV head (int8,
 // 28 heads over 196000 tokens, 4 KV heads: 37 us, 5.4 TB/s, and 4 the merge); a wave holds a block and asks for the next, 16 KB.  For
 // short sequences by its chain of round trips: arguments, length, codes (one head of 1568 tokens 4.3 us, merge 2.2).
 // grid (splits, H, B).
 template <int NT, int CODE, int W, class TREE>
-__device__ __forceinline__ void few_rows(const C8Attn a, const TREE tree) {
+__device__ __forceinline__ void few_rows(const C8Attn a) {
   const int b = blockIdx.z, h = blockIdx.y, sp = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int x = lane & 15, kb = lane >> 4;
@@ -487,8 +500,24 @@ __device__ __forceinline__ void few_rows(const C8Attn a, const TREE tree) {
   const size_t head = ((size_t)b * a.H + h) * a.nbc;
   Rows<NT> r;
   Block f, g;
+  __shared__ f4 so[W][16][D / 4 + 1];
   if (b0 < b1) load_block(f, a.kc, a.vc, a.km, a.vm, head + b0, lane);      // (on its way while the queries are laid out)
+  // A drafted block, the wave's last work, is asked for now too and waits in LDS (asked for at its turn: 48 rows of 16
+  // sequences 27.7 us).  NT tiles have at most two; a workgroup's second buffer is for the one that is not the last.
+  constexpr int BUFS = TREE::ON ? NT == 1 ? 1 : 2 : 0;
+  __shared__ u32x4 tree_keys[BUFS ? BUFS : 1][BUFS ? 512 : 1];
+  auto tree_block = [&] {
+    if constexpr (TREE::ON) return TreeBlock<typename TREE::Type, (W > 4), NT>{};
+    else return 0;
+  }();
+  const int first = max(b0, nb), buf = BUFS == 2 && first + 1 < blocks ? 1 : 0;
+  if constexpr (TREE::ON) {
+    if (first < end) tree_block.ask(a, b, h, rows, nq, first - nb, lane);
+  }
   load_rows<NT>(r, a, b, h, 0, rows, TREE::ON ? max(len, 1) : len, nq, lane);
+  if constexpr (TREE::ON) {
+    if (first < end) tree_block.put(tree_keys[buf], reinterpret_cast<u32x4*>(so[w]), lane);
+  }
   uint32_t vmost = 0;                      // the largest magnitude so far
   if (b0 < b1) {
     for (int i = b0; i < b1; ++i) {
@@ -501,12 +530,26 @@ __device__ __forceinline__ void few_rows(const C8Attn a, const TREE tree) {
       f = g;
     }
   }
-  __shared__ f4 so[W][16][D / 4 + 1];
   if constexpr (TREE::ON) {
+    const u32x4* keys = tree_keys[buf];
+    const u32x4* values = reinterpret_cast<const u32x4*>(so[w]);
 #pragma unroll 1
-    for (int i = max(b0, nb); i < end; ++i)
-      take_tree_alone<typename TREE::Type, CODE, (W > 4)>(r, tree, a, b, h, rows, nq, i - nb, __float_as_uint(kLevel<CODE>) + FAR < vmost,
-                                                 reinterpret_cast<u32x4*>(so[w]), lane);
+    for (int i = first; i < end; ++i) {
+      if (i > first) {
+        tree_block.ask(a, b, h, rows, nq, i - nb, lane);
+        tree_block.put(tree_keys[buf], reinterpret_cast<u32x4*>(so[w]), lane);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      auto op = [&](const u32x4* at) {
+        Op o;
+        o.q = at[lane];
+        return o;
+      };
+      take_tree<typename TREE::Type, CODE>(
+          r, [&](int tt, int j) { return op(keys + (4 * tt + j) * 64); }, [&](int c) { return op(values + c * 64); }, tree_block.sees,
+          __float_as_uint(kLevel<CODE>) + FAR < vmost, lane);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
   }
   // the waves' sums, a tile of rows at a time
   __shared__ float sm[W][16], sl[W][16];
@@ -558,7 +601,7 @@ __device__ __forceinline__ void few_rows(const C8Attn a, const TREE tree) {
 // grid (tiles of rows x splits x B x H), heads fastest: the tiles that see most come first, and what shares a head's
 // codes runs at the same time, where the heads divide the eight dies' turns on the same die.
 template <int NT, int CODE, class TREE>
-__device__ __forceinline__ void many_rows(const C8Attn a, int tiles, const TREE tree) {
+__device__ __forceinline__ void many_rows(const C8Attn a, int tiles) {
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int x = lane & 15, kb = lane >> 4;
   int at = blockIdx.x;
@@ -612,8 +655,52 @@ __device__ __forceinline__ void many_rows(const C8Attn a, int tiles, const TREE 
     ask_v(b0);
     ask_k(b0 + 1);
   }
+  // drafted tokens: each wave lays a quarter of a block out in LDS, keys as the codes above, values of lane group w.  The first
+  // block is asked for now and waits there; the others are asked for a block ahead, when the cached tokens are done (and the
+  // first too where three tiles a wave have no registers for it: 196000 tokens, 64 nodes 453 us with those spilled, 330 so).
+  constexpr bool EARLY = TREE::ON && NT < 3;
+  const int d0 = max(b0 - nb, 0), d1 = end - nb;
+  __shared__ Op tree_ops[EARLY ? 16 : 1][64];
+  __shared__ uint32_t tree_sees[2][4][NT][16];
+  u32x4 tk[2];
+  uint32_t tv[8], ts[NT];
+  auto ask_tree = [&](int i) {
+    if constexpr (TREE::ON) {
+      typedef typename TREE::Type T;
+      const TREE tree = TREE::argument();
+      int seq = b, head = h;
+      asm volatile("" : "+s"(seq), "+s"(head));          // (addresses are made again at every block: not kept over the cached tokens)
+      const char* K = tree.K.data + seq * tree.K.sb + head * tree.K.sh;
+      const char* V = tree.V.data + seq * tree.V.sb + head * tree.V.sh;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) tk[e] = tree_key<T>(K, tree.K.st, i * G + 16 * (w >> 1) + x, 2 * (w & 1) + e, nq, kb);
+      tree_values<T>(tv, V, tree.V.st, i * G, w, nq, lane);
+      load_sees(ts, tree, a, b, row0, rows, nq, i, lane);
+    }
+  };
+  auto put_tree = [&](Op(*to)[64], int i) {
+    if constexpr (TREE::ON) {
+      typedef typename TREE::Type T;
+      us2 m = most_of<T>(us2{0, 0}, tv);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) m = __builtin_elementwise_max(m, __builtin_bit_cast(us2, tk[e >> 2][e & 3] & 0x7fff7fffu));
+      if (beyond<T>(m)) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { tv[e] = held<T>(tv[e]); tk[e >> 2][e & 3] = held<T>(tk[e >> 2][e & 3]); }
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) to[2 * w + e][lane].q = tk[e];
+      put_values(&to[8][0].q, tv, w, lane);
+      if (kb == 0) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) tree_sees[i & 1][w][t][x] = ts[t];
+      }
+    }
+  };
+  if (EARLY && d0 < d1) ask_tree(d0);
   Rows<NT> r;
   load_rows<NT>(r, a, b, h, row0, rows, TREE::ON ? max(len, 1) : len, nq, lane);
+  if (EARLY && d0 < d1) put_tree(tree_ops, d0);
   f4 s[NT][2];
   Op p[NT], n0, n1;
   float al[NT];
@@ -784,39 +871,23 @@ __device__ __forceinline__ void many_rows(const C8Attn a, int tiles, const TREE 
     }
   }
   if constexpr (TREE::ON) {
-    // drafted tokens: each wave lays a quarter of a block out in LDS, keys as the codes above, values of lane group w
-    typedef typename TREE::Type T;
-    const char* K = tree.K.data + b * tree.K.sb + h * tree.K.sh;
-    const char* V = tree.V.data + b * tree.V.sb + h * tree.V.sh;
-    const int e0 = max(b0 - nb, 0), e1 = end - nb;
-    u32x4 k[2];
-    uint32_t v[8], sees[NT];
-    auto ask = [&](int i) {
-#pragma unroll
-      for (int e = 0; e < 2; ++e) k[e] = tree_key<T>(K, tree.K.st, i * G + 16 * (w >> 1) + x, 2 * (w & 1) + e, nq, kb);
-      tree_values<T>(v, V, tree.V.st, i * G, w, nq, lane);
-    };
-    if (e0 < e1) ask(e0);
+    if (!EARLY && d0 < d1) {
+      ask_tree(d0);
+      hand_over();                         // (the last cached block's operands have been read)
+      put_tree(ops[d0 & 1], d0);
+    }
 #pragma unroll 1
-    for (int i = e0; i < e1; ++i) {
-      us2 m = most_of<T>(us2{0, 0}, v);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) m = __builtin_elementwise_max(m, __builtin_bit_cast(us2, k[e >> 2][e & 3] & 0x7fff7fffu));
-      if (beyond<T>(m)) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) { v[e] = held<T>(v[e]); k[e >> 2][e & 3] = held<T>(k[e >> 2][e & 3]); }
-      }
-      load_sees(sees, tree, a, b, row0, rows, nq, i, lane);
-      if (i == e0) hand_over();            // (the last cached block's operands have been read)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) ops[i & 1][2 * w + e][lane].q = k[e];
-      put_values(&ops[i & 1][8][0].q, v, w, lane);
-      if (i + 1 < e1) ask(i + 1);
+    for (int i = d0; i < d1; ++i) {
+      if (i + 1 < d1) ask_tree(i + 1);
       hand_over();
-      const Op(*o)[64] = ops[i & 1];
-      take_tree<T, CODE>(
+      const Op(*o)[64] = EARLY && i == d0 ? tree_ops : ops[i & 1];
+      uint32_t sees[NT];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) sees[t] = tree_sees[i & 1][w][t][x];
+      take_tree<typename TREE::Type, CODE>(
           r, [&](int tt, int j) { return o[4 * tt + j][lane]; }, [&](int c) { return o[8 + c][lane]; }, sees,
           __float_as_uint(kLevel<CODE>) + FAR < vmost, lane);
+      if (i + 1 < d1) put_tree(ops[(i + 1) & 1], i + 1);
     }
   }
 #pragma unroll

@@ -6,12 +6,12 @@ namespace vidkv {
 
 template <int NT, int CODE, int W>
 __global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : NT < 3 ? 2 : 1) void c8_few_kernel(C8Attn a) {
-  few_rows<NT, CODE, W>(a, NoTree{});
+  few_rows<NT, CODE, W, NoTree>(a);
 }
 
 template <int NT, int CODE>
 __global__ __launch_bounds__(256, 2) void c8_many_kernel(C8Attn a, int tiles) {
-  many_rows<NT, CODE>(a, tiles, NoTree{});
+  many_rows<NT, CODE, NoTree>(a, tiles);
 }
 
 // out of the splits' partials.  A row is taken by 32 SL threads, 32 channel quads x SL slices of its splits, eight

@@ -10,13 +10,13 @@
 namespace vidkv {
 
 template <int NT, int CODE, int W, class T>
-__global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : NT < 3 ? 2 : 1) void c8_tree_few_kernel(C8Attn a, Tree<T> tree) {
-  few_rows<NT, CODE, W>(a, tree);
+__global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : NT < 3 ? 2 : 1) void c8_tree_few_kernel(C8Attn a, Tree<T>) {
+  few_rows<NT, CODE, W, Tree<T>>(a);
 }
 
 template <int NT, int CODE, class T>
-__global__ __launch_bounds__(256, 2) void c8_tree_many_kernel(C8Attn a, Tree<T> tree, int tiles) {
-  many_rows<NT, CODE>(a, tiles, tree);
+__global__ __launch_bounds__(256, 2) void c8_tree_many_kernel(C8Attn a, Tree<T>, int tiles) {
+  many_rows<NT, CODE, Tree<T>>(a, tiles);
 }
 
 hipError_t launch_c8_tree(const C8Geom& g, int layer, int n, float scale, const vidkv_view* q, const vidkv_view* K, const vidkv_view* V,
