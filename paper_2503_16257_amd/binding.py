@@ -206,6 +206,8 @@ def _load_native(L):
     m.bind8(*(C.cast(f, C.c_void_p).value for f in (
         L.vidkv_rotary_apply, L.vidkv_cache8_write, L.vidkv_cache8_read, L.vidkv_cache8_attention)),
         VidkvRotary, VidkvCache8)
+    m.bind_tree(*(C.cast(f, C.c_void_p).value for f in (
+        L.vidkv_tree_masks, L.vidkv_cache8_tree_attention, L.vidkv_tree_verify, L.vidkv_cache8_append_path)))
     return m
 
 
@@ -578,6 +580,10 @@ def tree_masks(parents, masks, base=None, positions=None, count=None, stream=Non
     base [B] int32, positions [n_axes,B,n] int32.  parents None: chains, of the masks' sizes.  count[b]: nodes that there are
     (None: all n)."""
     L = _lib or lib()
+    if _native is not None:
+        st = _native.tree_masks(parents, masks, base, positions, count, _stream, stream)
+        if st is not None:
+            return _check(st, "vidkv_tree_masks")
     if not isinstance(masks, _Tensor) or masks.dim() != 3:
         raise ValueError("masks: expected a tensor [batch, nodes, words]")
     B, n = masks.shape[0], masks.shape[1]
@@ -597,6 +603,10 @@ def cache8_tree_attention(p: VidkvCache8, layer: int, cache, q, K, V, masks, out
     nodes of K, V [B,Hkv,n,128] that masks [B,n,words] int64 has for each -> out.  The workspace is that of
     cache8_attention (cache8_workspace_bytes(p, n))."""
     L = _lib or lib()
+    if _native is not None:
+        st = _native.cache8_tree_attention(p, layer, cache, q, K, V, masks, out, length, workspace, count, _stream, stream)
+        if st is not None:
+            return _check(st, "vidkv_cache8_tree_attention")
     n = q.shape[2] if isinstance(q, _Tensor) and q.dim() == 4 else -1
     shape, kv = (p.batch, p.n_q_heads, n, 128), (p.batch, p.n_kv_heads, n, 128)
     vq, vk, vv, vo = _view(q, "q", shape), _view(K, "K", kv), _view(V, "V", kv), _view(out, "out", shape, True)
@@ -636,6 +646,11 @@ def tree_verify(target, tokens, uniform, path, accepted, next_token, workspace, 
     draft [B,n,vocab]: what the children of each node were drawn from, with `distinct` without putting back; None: they are no
     random ones.  parents None: chains."""
     L = _lib or lib()
+    if _native is not None:
+        st = _native.tree_verify(target, tokens, uniform, path, accepted, next_token, workspace, draft, parents, count, distinct,
+                                 _stream, stream)
+        if st is not None:
+            return _check(st, "vidkv_tree_verify")
     B, n = _nodes(tokens, "tokens")
     V = target.shape[2] if isinstance(target, _Tensor) and target.dim() == 3 else -1
     t, d = _rows(target, "target", (B, n, V)), _rows(draft, "draft", (B, n, V))
@@ -651,6 +666,10 @@ def cache8_append_path(p: VidkvCache8, cache, K, V, path, accepted, start, strea
     """vidkv_cache8_append_path: of K, V [n_layers,B,Hkv,n,128] fp16 / bf16 the nodes path[b][:accepted[b]] coded as tokens
     start[b].. of every layer."""
     L = _lib or lib()
+    if _native is not None:
+        st = _native.cache8_append_path(p, cache, K, V, path, accepted, start, _stream, stream)
+        if st is not None:
+            return _check(st, "vidkv_cache8_append_path")
     B, n = _nodes(path, "path")
     v, layer = [], []
     for t, name in ((K, "K"), (V, "V")):

@@ -19,10 +19,32 @@ __global__ __launch_bounds__(256, 2) void c8_tree_many_kernel(C8Attn a, Tree<T>,
   many_rows<NT, CODE, Tree<T>>(a, tiles);
 }
 
+// The attention's plan, with fewer splits where its last workgroups would be a round of their own: it allows the next more
+// than two a compute unit, and a tree's rows are seldom a divisor of them (64 nodes x 7 heads x 4 over 196000 tokens, three tiles: 43 splits
+// are 516 workgroups, 329 us; 42 are 504, 220).  More than the plan's are not taken, so that its workspace does.  Costs as in
+// c8_plan(); a round is two workgroups a compute unit, the last one's are alone if they are no more than one.  (Trees of very
+// different sizes leave tiles without rows, whose workgroups end at once: two of 128 to 256 nodes, 25088 tokens, 7 splits 187 us, 6
+// by this rule 206; both of 256 nodes 296 and 214.)
+static C8Plan tree_plan(const C8Geom& g, int n) {
+  C8Plan p = c8_plan(g, n);
+  if (p.few) return p;
+  const long long heads = (long long)g.H * g.B, wgs = p.tiles * heads, cu = device_cu_count();
+  const float alone = 0.8f + 0.1f * p.nt, beside = p.nt == 1 ? 1.0f : p.nt == 2 ? 1.25f : 1.65f;
+  const float blocks = (float)(g.nbc + (n + G - 1) / G), row_us = (float)heads * n * g.rep * (2 * 528 / 5e6f);
+  float least = 0.0f;
+  for (int k = 1, most = p.splits; k <= most; ++k) {
+    const long long all = wgs * k, rest = all % (2 * cu);
+    const float round = (float)(all / (2 * cu)) * beside + (rest == 0 ? 0.0f : rest <= cu ? alone : beside);
+    const float us = blocks / k * round + (k > 1 ? 4.0f + row_us * k : 0.0f);
+    if (k == 1 || us < least) { least = us; p.splits = k; }
+  }
+  return p;
+}
+
 hipError_t launch_c8_tree(const C8Geom& g, int layer, int n, float scale, const vidkv_view* q, const vidkv_view* K, const vidkv_view* V,
                           const uint64_t* mask, const uint8_t* cache, const int32_t* length, const int32_t* count,
                           const vidkv_view* out, void* ws, hipStream_t st) {
-  const C8Plan p = c8_plan(g, n);
+  const C8Plan p = tree_plan(g, n);
   const C8Attn a = c8_args(g, p, layer, n, 0, scale, q, cache, length, count, out, ws);
   auto go = [&](auto t, auto code) {
     using T = decltype(t);

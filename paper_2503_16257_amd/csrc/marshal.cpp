@@ -26,6 +26,10 @@ decltype(&vidkv_rotary_apply) g_rotary;
 decltype(&vidkv_cache8_write) g_write8;
 decltype(&vidkv_cache8_read) g_read8;
 decltype(&vidkv_cache8_attention) g_attend8;
+decltype(&vidkv_tree_masks) g_masks;
+decltype(&vidkv_cache8_tree_attention) g_tree8;
+decltype(&vidkv_tree_verify) g_verify;
+decltype(&vidkv_cache8_append_path) g_append8;
 PyTypeObject* g_params_type;         // binding.VidkvParams
 PyTypeObject* g_side_type;           // binding.VidkvSideStream
 PyTypeObject* g_rotary_type;         // binding.VidkvRotary
@@ -405,6 +409,173 @@ PyObject* bind8(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
+// ---- trees of drafted tokens ----
+// A contiguous device tensor of shape [B, n].
+bool table(PyObject* o, int dev, c10::ScalarType t, int64_t B, int64_t n, bool none_ok, void** ptr) {
+  return tensor_here(o, dev, t, {B, n}, none_ok, ptr);
+}
+
+// binding.py's _rows: [B, n, vocab] of any strides, a row's entries next to each other.
+bool rows(PyObject* o, int dev, int64_t B, int64_t n, int64_t V, vidkv_rows* r) {
+  const at::Tensor* x = here(o, dev);
+  if (!x || x->dim() != 3) return false;
+  const auto size = x->sizes(), stride = x->strides();
+  if (size[0] != B || size[1] != n || size[2] != V || (stride[2] != 1 && V > 1)) return false;
+  switch (x->scalar_type()) {
+    case at::kHalf: r->dtype = VIDKV_F16; break;
+    case at::kBFloat16: r->dtype = VIDKV_BF16; break;
+    case at::kFloat: r->dtype = VIDKV_F32; break;
+    default: return false;
+  }
+  r->data = x->data_ptr();
+  r->stride_batch = B > 1 ? stride[0] : 0;
+  r->stride_row = n > 1 ? stride[1] : 0;
+  return true;
+}
+
+// A plain tensor's sizes, `nd` of them above zero, or false.
+bool sizes(PyObject* o, int nd, int64_t* size) {
+  if (!THPVariable_CheckExact(o)) return false;
+  const at::Tensor& x = THPVariable_Unpack(o);
+  if (!x.defined() || x.dim() != nd) return false;
+  for (int i = 0; i < nd; ++i) {
+    size[i] = x.size(i);
+    if (size[i] <= 0 || size[i] > INT32_MAX) return false;
+  }
+  return true;
+}
+
+// (parents, masks, base, positions, count, stream function, stream)
+PyObject* masks(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 7 || !g_masks) Py_RETURN_NONE;
+  return guarded([&]() -> PyObject* {
+    int64_t m[3], x[3] = {0, 0, 0};
+    void *parents, *words, *base, *pos, *count;
+    const bool placed = a[3] != Py_None;
+    if (!sizes(a[1], 3, m) || placed != (a[2] != Py_None) || (placed && !sizes(a[3], 3, x))) Py_RETURN_NONE;
+    const int dev = current_device();
+    if (!table(a[0], dev, at::kInt, m[0], m[1], true, &parents) ||
+        !tensor_here(a[1], dev, at::kLong, {m[0], m[1], (m[1] + 63) / 64}, false, &words) ||
+        !tensor_here(a[2], dev, at::kInt, {m[0]}, !placed, &base) ||
+        !tensor_here(a[3], dev, at::kInt, {x[0], m[0], m[1]}, !placed, &pos) || !tensor_here(a[4], dev, at::kInt, {m[0]}, true, &count))
+      Py_RETURN_NONE;
+    return enqueue(a[5], a[6], [&](void* s) {
+      return g_masks((int32_t)m[0], (int32_t)m[1], static_cast<const int32_t*>(parents), static_cast<const int32_t*>(count),
+                     static_cast<uint64_t*>(words), (int32_t)x[0], static_cast<const int32_t*>(base), static_cast<int32_t*>(pos), s);
+    });
+  });
+}
+
+// (cache8, layer, cache, q, K, V, masks, out, length, workspace, count, stream function, stream)
+PyObject* tree8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 13 || !g_tree8) Py_RETURN_NONE;
+  return guarded([&]() -> PyObject* {
+    const Struct ps(a[0], g_cache8_type, sizeof(vidkv_cache8));
+    const auto* p = static_cast<const vidkv_cache8*>(ps.get());
+    int32_t layer;
+    int64_t B, h, t;
+    void *cache, *words, *length, *count, *ws;
+    size_t bytes = 0, wsb = 0;
+    vidkv_view q, K, V, out;
+    if (!p || !integer(a[1], &layer) || !dims(a[3], &B, &h, &t)) Py_RETURN_NONE;
+    const int dev = current_device();
+    if (!view(a[3], dev, p->batch, p->n_q_heads, t, 128, false, &q) || !view(a[4], dev, p->batch, p->n_kv_heads, t, 128, false, &K) ||
+        !view(a[5], dev, p->batch, p->n_kv_heads, t, 128, false, &V) || !view(a[7], dev, p->batch, p->n_q_heads, t, 128, true, &out) ||
+        !tensor_here(a[6], dev, at::kLong, {p->batch, t, (t + 63) / 64}, false, &words) ||
+        !tensor_here(a[2], dev, at::kByte, {}, false, &cache, &bytes) ||
+        !tensor_here(a[8], dev, at::kInt, {p->batch}, false, &length) || !tensor_here(a[9], dev, at::kByte, {}, false, &ws, &wsb) ||
+        !tensor_here(a[10], dev, at::kInt, {p->batch}, true, &count))
+      Py_RETURN_NONE;
+    return enqueue(a[11], a[12], [&](void* s) {
+      return g_tree8(p, layer, (int32_t)t, &q, &K, &V, static_cast<const uint64_t*>(words), cache, bytes,
+                     static_cast<const int32_t*>(length), static_cast<const int32_t*>(count), &out, ws, wsb, s);
+    });
+  });
+}
+
+// (target, tokens, uniform, path, accepted, next, workspace, draft, parents, count, distinct, stream function, stream)
+PyObject* verify(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 13 || !g_verify) Py_RETURN_NONE;
+  return guarded([&]() -> PyObject* {
+    int64_t m[3];
+    int32_t distinct;
+    vidkv_rows target, draft;
+    void *tokens, *uniform, *path, *accepted, *next, *ws, *parents, *count;
+    size_t wsb = 0;
+    const bool drawn = a[7] != Py_None;
+    if (!sizes(a[0], 3, m) || !boolean(a[10], &distinct)) Py_RETURN_NONE;
+    const int dev = current_device();
+    if (!rows(a[0], dev, m[0], m[1], m[2], &target) || (drawn && !rows(a[7], dev, m[0], m[1], m[2], &draft)) ||
+        !table(a[1], dev, at::kInt, m[0], m[1], false, &tokens) || !table(a[2], dev, at::kFloat, m[0], m[1], false, &uniform) ||
+        !table(a[3], dev, at::kInt, m[0], m[1], false, &path) || !tensor_here(a[4], dev, at::kInt, {m[0]}, false, &accepted) ||
+        !tensor_here(a[5], dev, at::kInt, {m[0]}, false, &next) || !tensor_here(a[6], dev, at::kByte, {}, false, &ws, &wsb) ||
+        !table(a[8], dev, at::kInt, m[0], m[1], true, &parents) || !tensor_here(a[9], dev, at::kInt, {m[0]}, true, &count))
+      Py_RETURN_NONE;
+    return enqueue(a[11], a[12], [&](void* s) {
+      return g_verify((int32_t)m[0], (int32_t)m[1], (int32_t)m[2], &target, drawn ? &draft : nullptr, distinct,
+                      static_cast<const int32_t*>(tokens), static_cast<const int32_t*>(parents), static_cast<const int32_t*>(count),
+                      static_cast<const float*>(uniform), static_cast<int32_t*>(path), static_cast<int32_t*>(accepted),
+                      static_cast<int32_t*>(next), ws, wsb, s);
+    });
+  });
+}
+
+// A view of layer 0 of [L, B, heads, n, 128], and the stride from layer to layer.
+bool layers(PyObject* o, int dev, const vidkv_cache8* p, int64_t n, vidkv_view* v, int64_t* stride) {
+  const at::Tensor* x = here(o, dev);
+  if (!x || x->dim() != 5) return false;
+  const auto size = x->sizes(), st = x->strides();
+  if (size[0] != p->n_layers || size[1] != p->batch || size[2] != p->n_kv_heads || size[3] != n || size[4] != 128 || st[4] != 1) return false;
+  switch (x->scalar_type()) {
+    case at::kHalf: v->dtype = VIDKV_F16; break;
+    case at::kBFloat16: v->dtype = VIDKV_BF16; break;
+    default: return false;
+  }
+  v->data = x->data_ptr();
+  v->stride_batch = size[1] > 1 ? st[1] : 0;
+  v->stride_head = size[2] > 1 ? st[2] : 0;
+  v->stride_token = size[3] > 1 ? st[3] : 0;
+  *stride = size[0] > 1 ? st[0] : 0;
+  return true;
+}
+
+// (cache8, cache, K, V, path, accepted, start, stream function, stream)
+PyObject* append8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 9 || !g_append8) Py_RETURN_NONE;
+  return guarded([&]() -> PyObject* {
+    const Struct ps(a[0], g_cache8_type, sizeof(vidkv_cache8));
+    const auto* p = static_cast<const vidkv_cache8*>(ps.get());
+    int64_t m[2], ks, vs;
+    void *cache, *path, *accepted, *start;
+    size_t bytes = 0;
+    vidkv_view K, V;
+    if (!p || !sizes(a[4], 2, m)) Py_RETURN_NONE;
+    const int dev = current_device();
+    if (!layers(a[2], dev, p, m[1], &K, &ks) || !layers(a[3], dev, p, m[1], &V, &vs) ||
+        !table(a[4], dev, at::kInt, p->batch, m[1], false, &path) || !tensor_here(a[5], dev, at::kInt, {p->batch}, false, &accepted) ||
+        !tensor_here(a[6], dev, at::kInt, {p->batch}, false, &start) || !tensor_here(a[1], dev, at::kByte, {}, false, &cache, &bytes))
+      Py_RETURN_NONE;
+    return enqueue(a[7], a[8], [&](void* s) {
+      return g_append8(p, (int32_t)m[1], &K, ks, &V, vs, static_cast<const int32_t*>(path), static_cast<const int32_t*>(accepted),
+                       static_cast<const int32_t*>(start), cache, bytes, s);
+    });
+  });
+}
+
+// (addresses of vidkv_tree_masks, vidkv_cache8_tree_attention, vidkv_tree_verify, vidkv_cache8_append_path; behind bind8)
+PyObject* bind_tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  void* f[4];
+  if (n != 4 || !handle(a[0], &f[0]) || !handle(a[1], &f[1]) || !handle(a[2], &f[2]) || !handle(a[3], &f[3])) {
+    PyErr_SetString(PyExc_TypeError, "bind_tree: four addresses");
+    return nullptr;
+  }
+  g_masks = reinterpret_cast<decltype(g_masks)>(f[0]);
+  g_tree8 = reinterpret_cast<decltype(g_tree8)>(f[1]);
+  g_verify = reinterpret_cast<decltype(g_verify)>(f[2]);
+  g_append8 = reinterpret_cast<decltype(g_append8)>(f[3]);
+  Py_RETURN_NONE;
+}
+
 PyMethodDef methods[] = {
     {"decode_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(decode)), METH_FASTCALL, nullptr},
     {"decode_attention_noalloc", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(decode_noalloc)), METH_FASTCALL, nullptr},
@@ -413,6 +584,11 @@ PyMethodDef methods[] = {
     {"cache8_write", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(write8)), METH_FASTCALL, nullptr},
     {"cache8_read", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(read8)), METH_FASTCALL, nullptr},
     {"cache8_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(attend8)), METH_FASTCALL, nullptr},
+    {"tree_masks", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(masks)), METH_FASTCALL, nullptr},
+    {"cache8_tree_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(tree8)), METH_FASTCALL, nullptr},
+    {"tree_verify", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(verify)), METH_FASTCALL, nullptr},
+    {"cache8_append_path", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(append8)), METH_FASTCALL, nullptr},
+    {"bind_tree", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(bind_tree)), METH_FASTCALL, nullptr},
     {"bind8", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(bind8)), METH_FASTCALL, nullptr},
     {"bind", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(bind)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
