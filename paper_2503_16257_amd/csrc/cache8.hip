@@ -9,7 +9,10 @@ namespace vidkv {
 
 template <class T, int CODE, bool ROT>
 __global__ __launch_bounds__(256) void c8_write_kernel(C8Write a) {
-  write_block<T, CODE, ROT>(a, InOrder{});
+  ask_arguments(a);
+  if constexpr (ROT) asm volatile("" :: "s"(a.rot.pos), "s"(a.rot.rows), "s"(a.rot.rot_dim), "s"(a.rot.adjacent), "s"(a.n_axes));
+  const int b = blockIdx.z;
+  write_block<T, CODE, ROT>(a, InOrder{}, b, blockIdx.y, 0, blockIdx.x, a.start[b], a.count ? min(a.count[b], a.n) : a.n, nullptr);
 }
 
 hipError_t launch_c8_write(const C8Geom& g, int layer, int n, const vidkv_view* K, const vidkv_view* V,

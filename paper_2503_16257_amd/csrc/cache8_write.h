@@ -49,7 +49,7 @@ struct InOrder {
 struct Path {
   static constexpr bool PICKED = true;
   const int32_t* path;                     // [B][n]
-  int B, reach;                            // reach: blocks that a sequence's tokens can touch
+  int B;
   long long k_layer, v_layer;              // strides in bytes
 };
 
@@ -65,39 +65,17 @@ __device__ __forceinline__ uint32_t lane_xor8(uint32_t v) {
 // is known.  8 x 4 heads x 12544 tokens in fp16: 67 us for 308 MB, 4.6 TB/s; the vector units are the second bound, 9
 // instructions an element of which the exact quotient is 4 (with a branch a row, values in 8-byte stores at every second place
 // and maxima in float32: 84 us).  One token of 64 sequences, turned: 5.5 us.  grid (blocks a sequence can reach, H, B).
+// Here: block `nth` of those that `count` new tokens of sequence b reach from `start` on, if it is one of them; nodes: the tokens' rows, if
+// they are picked.
 template <class T, int CODE, bool ROT, class ROWS>
-__device__ __forceinline__ void write_block(const C8Write a, const ROWS rows) {
-  // (all arguments in one round trip; left to itself the compiler asks for each where it is used)
-  asm volatile("" :: "s"(a.K.data), "s"(a.K.sb), "s"(a.K.sh), "s"(a.K.st), "s"(a.V.data), "s"(a.V.sb), "s"(a.V.sh), "s"(a.V.st),
-               "s"(a.start), "s"(a.count), "s"(a.kc), "s"(a.vc), "s"(a.km), "s"(a.vm), "s"(a.H), "s"(a.nbc), "s"(a.cap), "s"(a.n));
-  if constexpr (ROT) asm volatile("" :: "s"(a.rot.pos), "s"(a.rot.rows), "s"(a.rot.rot_dim), "s"(a.rot.adjacent), "s"(a.n_axes));
+__device__ __forceinline__ void write_block(const C8Write& a, const ROWS& rows, int b, int h, int layer, int nth, int start, int count,
+                                            const int* nodes) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  int b = blockIdx.z, h = blockIdx.y, nth = blockIdx.x, layer = 0;         // nth: block of the sequence's new tokens
-  if constexpr (ROWS::PICKED) {
-    int at = blockIdx.x;
-    nth = at % rows.reach; at /= rows.reach;
-    h = at % a.H; at /= a.H;
-    b = at % rows.B;
-    layer = at / rows.B;
-  }
-  const int start = a.start[b];
-  int count = a.count ? min(a.count[b], a.n) : a.n;
   if (start < 0 || count <= 0) return;
   const long long first = (long long)(start / G + (long long)nth) * G;
-  if (first >= (long long)start + count || first >= a.cap) return;
-  __shared__ int nodes[ROWS::PICKED ? 256 : 1];
-  if constexpr (ROWS::PICKED) {            // the path ends before the first entry that is no node
-    __shared__ int bad[4];
-    const int node = tid < count ? rows.path[(size_t)b * a.n + tid] : 0;
-    nodes[tid] = node;
-    const uint64_t out = __ballot(node < 0 || node >= a.n);
-    if (lane == 0) bad[w] = out ? 64 * w + __builtin_ctzll(out) : 256;
-    __syncthreads();
-    count = min(min(min(bad[0], bad[1]), min(bad[2], bad[3])), count);
-    if (count <= 0 || first >= (long long)start + count) return;
-  }
   const long long end = (long long)start + count;
+  if (first >= end || first >= a.cap) return;
   const char* kin = a.K.data + b * a.K.sb + h * a.K.sh;
   const char* vin = a.V.data + b * a.V.sb + h * a.V.sh;        // (row addresses are the wave's: scalar)
   int seq = b;                             // of the cache: a layer's sequences lie behind those of the layer before it
@@ -146,7 +124,7 @@ __device__ __forceinline__ void write_block(const C8Write a, const ROWS rows) {
   u32x4 vold{};
   if (begun) {
     ko = a.km[blk]; vo = a.vm[blk];
-    k0 = *pk0; k1 = *pk1;
+    if constexpr (!ROWS::PICKED) { k0 = *pk0; k1 = *pk1; }
   }
   if (!whole) vold = *pv;
   auto sines = [&](int token, int pair, float* co, float* si) {           // of new token `token` of the sequence
@@ -238,6 +216,7 @@ __device__ __forceinline__ void write_block(const C8Write a, const ROWS rows) {
     *pk0 = p;
     *pk1 = q;
   } else if (kt < start && ka > ko) {      // (only in a begun block)
+    if constexpr (ROWS::PICKED) { k0 = *pk0; k1 = *pk1; }
     *pk0 = uint2{again(k0.x, ko, ka, rk), again(k0.y, ko, ka, rk)};
     *pk1 = uint2{again(k1.x, ko, ka, rk), again(k1.y, ko, ka, rk)};
   }
@@ -272,6 +251,12 @@ __device__ __forceinline__ void write_block(const C8Write a, const ROWS rows) {
     }
   }
   *pv = r;
+}
+
+// All arguments of a writing kernel in one round trip; left to itself the compiler asks for each where it is used.
+__device__ __forceinline__ void ask_arguments(const C8Write& a) {
+  asm volatile("" :: "s"(a.K.data), "s"(a.K.sb), "s"(a.K.sh), "s"(a.K.st), "s"(a.V.data), "s"(a.V.sb), "s"(a.V.sh), "s"(a.V.st),
+               "s"(a.start), "s"(a.count), "s"(a.kc), "s"(a.vc), "s"(a.km), "s"(a.vm), "s"(a.H), "s"(a.nbc), "s"(a.cap), "s"(a.n));
 }
 
 // Blocks of a sequence that its n new tokens can touch, wherever they start; those behind the capacity are dropped.
