@@ -213,7 +213,7 @@ vidkv_status vidkv_cache8_tree_attention(const vidkv_cache8* p, int32_t layer, i
   if (cache_bytes < g.total || ws_bytes < c8_attn_ws_need(g, n_nodes)) return VIDKV_ENOSPACE;
   if (!stream_on_current_device(static_cast<hipStream_t>(stream))) return VIDKV_EINVAL;
   const hipError_t e = launch_c8_tree(g, layer, n_nodes, p->softmax_scale, q, K, V, mask, static_cast<const uint8_t*>(cache), length,
-                                      count, out, ws, static_cast<hipStream_t>(stream));
+                                      count, out, ws, ws_bytes, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? VIDKV_OK : VIDKV_EHIP;
 }
 

@@ -598,19 +598,24 @@ __device__ __forceinline__ void few_rows(const C8Attn a) {
 // the rows that pad the last tile); 6272 over themselves, causal: 270 us, 1.04.  On the way there: each wave decoding for
 // itself from memory 902 and 750; the weights in a phase of their own 340 and 350; eight waves to a workgroup, half the
 // decoding each: the same.  32 x 32 x 16 products, which cost the vector units less, with 32 rows a wave: 460 and 355.
-// grid (tiles of rows x splits x B x H), heads fastest: the tiles that see most come first, and what shares a head's
-// codes runs at the same time, where the heads divide the eight dies' turns on the same die.
-template <int NT, int CODE, class TREE>
-__device__ __forceinline__ void many_rows(const C8Attn a, int tiles) {
+struct ManySpan {
+  int b, h, tile0;             // the workgroup's first row
+  int sp, splits;              // of the splits of its rows (the partials have a.splits)
+};
+template <class TREE, bool EARLY>
+struct ManyLds {
+  Op ops[2][16][64];           // 0..7: K, tile of tokens tt, channels j at 4 tt + j; 8..15: V, tile of channels
+  Op tree_ops[EARLY ? 16 : 1][64];
+  uint32_t tree_sees[2][4][TREE::ON ? 3 : 1][16];
+};
+template <int NT, int CODE, class TREE, class LDS>
+__device__ __forceinline__ void many_rows(const C8Attn a, const ManySpan span, LDS& lds) {
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int x = lane & 15, kb = lane >> 4;
-  int at = blockIdx.x;
-  const int h = at % a.H; at /= a.H;
-  const int b = at % a.B; at /= a.B;
-  const int sp = at % a.splits, tile = tiles - 1 - at / a.splits;
+  const int b = span.b, h = span.h, sp = span.sp;
   const int len = min(max(a.length[b], 0), a.cap);
   const int nq = a.q_count ? min(max(a.q_count[b], 0), a.n) : a.n;
-  const int rows = a.n * a.rep, tile0 = tile * 64 * NT, row0 = tile0 + w * 16 * NT;
+  const int rows = a.n * a.rep, tile0 = span.tile0, row0 = tile0 + w * 16 * NT;
   // tokens that the first row from `row` on sees, and those that the last of `n` rows does
   auto least = [&](int row) { return row / a.rep >= nq ? 0 : a.causal ? max(len - nq + row / a.rep + 1, 0) : len; };
   auto most = [&](int row, int n) {
@@ -619,10 +624,10 @@ __device__ __forceinline__ void many_rows(const C8Attn a, int tiles) {
   };
   const int all = least(row0), nb = (most(tile0, 64 * NT) + G - 1) / G;
   const int blocks = nb + (TREE::ON && tile0 / a.rep < nq ? (nq + G - 1) / G : 0);      // cached ones, then drafted ones
-  const int b0 = (int)((long long)sp * blocks / a.splits), end = (int)((long long)(sp + 1) * blocks / a.splits);
+  const int b0 = (int)((long long)sp * blocks / span.splits), end = (int)((long long)(sp + 1) * blocks / span.splits);
   const int b1 = TREE::ON ? min(end, nb) : end;
   const size_t head = ((size_t)b * a.H + h) * a.nbc;
-  __shared__ Op ops[2][16][64];            // 0..7: K, tile of tokens tt, channels j at 4 tt + j; 8..15: V, tile of channels
+  Op(&ops)[2][16][64] = lds.ops;
   // this wave's quarter: K piece w (tt = w >> 1, j = 2 (w & 1) and the next), V piece w (m = 2 w and the next)
   const uint8_t* kc = a.kc + head * C8REC + ((w >> 1) * 16 + x) * D + (w & 1) * 64 + kb * 16;
   const uint8_t* vc = a.vc + head * C8REC + w * 1024 + lane * 16;
@@ -660,8 +665,8 @@ __device__ __forceinline__ void many_rows(const C8Attn a, int tiles) {
   // first too where three tiles a wave have no registers for it: 196000 tokens, 64 nodes 453 us with those spilled, 330 so).
   constexpr bool EARLY = TREE::ON && NT < 3;
   const int d0 = max(b0 - nb, 0), d1 = end - nb;
-  __shared__ Op tree_ops[EARLY ? 16 : 1][64];
-  __shared__ uint32_t tree_sees[2][4][NT][16];
+  auto& tree_ops = lds.tree_ops;
+  auto& tree_sees = lds.tree_sees;
   u32x4 tk[2];
   uint32_t tv[8], ts[NT];
   auto ask_tree = [&](int i) {
@@ -907,6 +912,18 @@ __device__ __forceinline__ void many_rows(const C8Attn a, int tiles) {
       for (int m = 0; m < 8; ++m) put_out(a, b, h, row, 16 * m + 4 * kb, l != 0.0f ? r.o[t][m] * f : f4{0.f, 0.f, 0.f, 0.f});
     }
   }
+  if constexpr (TREE::ON) {
+    // fewer splits than the partials have: one of nothing for each behind them
+    if (a.po && sp + span.splits < a.splits) {
+      for (int i = tid; i < 64 * NT * (D / 4); i += 256) {
+        const int row = tile0 + i / (D / 4);
+        if (row >= rows) break;
+        const size_t at = (((size_t)b * a.H + h) * rows + row) * a.splits + sp + span.splits;
+        reinterpret_cast<f4*>(a.po)[at * (D / 4) + i % (D / 4)] = f4{0.f, 0.f, 0.f, 0.f};
+        if (i % (D / 4) == 0) { a.pml[2 * at] = NONE; a.pml[2 * at + 1] = 0.0f; }
+      }
+    }
+  }
 }
 
 // How a call is shared out.
@@ -917,6 +934,16 @@ struct C8Plan {
   int tiles, splits;
   int most;                    // rows shared out: the splits that there can be
 };
+// Workgroup `at` of tiles x splits x B x H, heads fastest: the tiles that see most come first, and what shares a head's codes runs at
+// the same time, where the heads divide the eight dies' turns on the same die.
+template <int NT>
+__device__ __forceinline__ ManySpan even_span(const C8Attn& a, int at, int tiles) {
+  const int h = at % a.H; at /= a.H;
+  const int b = at % a.B; at /= a.B;
+  const int sp = at % a.splits, tile = tiles - 1 - at / a.splits;
+  return ManySpan{b, h, tile * 64 * NT, sp, a.splits};
+}
+
 C8Plan c8_plan(const C8Geom& g, int n);
 // Arguments of a call whose plan it is, and the merge of its splits behind it (cache8_attn.hip).
 C8Attn c8_args(const C8Geom& g, const C8Plan& p, int layer, int n, int causal, float scale, const vidkv_view* q, const uint8_t* cache,

@@ -11,7 +11,8 @@ __global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : NT < 3 ? 2 : 1) void c8_few
 
 template <int NT, int CODE>
 __global__ __launch_bounds__(256, 2) void c8_many_kernel(C8Attn a, int tiles) {
-  many_rows<NT, CODE, NoTree>(a, tiles);
+  __shared__ ManyLds<NoTree, false> lds;
+  many_rows<NT, CODE, NoTree>(a, even_span<NT>(a, blockIdx.x, tiles), lds);
 }
 
 // out of the splits' partials.  A row is taken by 32 SL threads, 32 channel quads x SL slices of its splits, eight

@@ -6,6 +6,8 @@
 // launch and no pass of their own.
 #include "cache8_attn.h"
 #include "tree.h"
+#include <algorithm>
+#include <cmath>
 
 namespace vidkv {
 
@@ -16,42 +18,85 @@ __global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : NT < 3 ? 2 : 1) void c8_tre
 
 template <int NT, int CODE, class T>
 __global__ __launch_bounds__(256, 2) void c8_tree_many_kernel(C8Attn a, Tree<T>, int tiles) {
-  many_rows<NT, CODE, Tree<T>>(a, tiles);
+  __shared__ ManyLds<Tree<T>, (NT < 3)> lds;
+  many_rows<NT, CODE, Tree<T>>(a, even_span<NT>(a, blockIdx.x, tiles), lds);
 }
 
-// The attention's plan, with fewer splits where its last workgroups would be a round of their own: it allows the next more
-// than two a compute unit, and a tree's rows are seldom a divisor of them (64 nodes x 7 heads x 4 over 196000 tokens, three tiles: 43 splits
-// are 516 workgroups, 329 us; 42 are 504, 220).  More than the plan's are not taken, so that its workspace does.  Costs as in
-// c8_plan(); a round is two workgroups a compute unit, the last one's are alone if they are no more than one.  (Trees of very
-// different sizes leave tiles without rows, whose workgroups end at once: two of 128 to 256 nodes, 25088 tokens, 7 splits 187 us, 6
-// by this rule 206; both of 256 nodes 296 and 214.)
-static C8Plan tree_plan(const C8Geom& g, int n) {
-  C8Plan p = c8_plan(g, n);
-  if (p.few) return p;
-  const long long heads = (long long)g.H * g.B, wgs = p.tiles * heads, cu = device_cu_count();
-  const float alone = 0.8f + 0.1f * p.nt, beside = p.nt == 1 ? 1.0f : p.nt == 2 ? 1.25f : 1.65f;
-  const float blocks = (float)(g.nbc + (n + G - 1) / G), row_us = (float)heads * n * g.rep * (2 * 528 / 5e6f);
+// Rows that are some tiles of 192 and a rest of up to 128: the rest's workgroups have one or two tiles a wave, a block takes them
+// less time, and so the rest has fewer splits (`few` of a.splits).  Workgroups of the rest come first.
+template <int REST, int CODE, class T>
+__global__ __launch_bounds__(256, 2) void c8_tree_mixed_kernel(C8Attn a, Tree<T>, int full, int few) {
+  __shared__ ManyLds<Tree<T>, true> lds;
+  int at = blockIdx.x;
+  const int h = at % a.H; at /= a.H;
+  const int b = at % a.B; at /= a.B;
+  const bool rest = at < few;
+  ManySpan span{b, h, full * 192, at, few};
+  if (!rest) span = ManySpan{b, h, (at - few) % full * 192, (at - few) / full, a.splits};
+  asm volatile("" : "+s"(span.b), "+s"(span.h), "+s"(span.tile0), "+s"(span.sp), "+s"(span.splits));
+  if (rest) many_rows<REST, CODE, Tree<T>>(a, span, lds);
+  else many_rows<3, CODE, Tree<T>>(a, span, lds);
+}
+
+struct TreePlan {
+  C8Plan p;
+  int full, few;               // mixed: tiles of 192 rows, splits of the rest; few = 0: tiles of one size
+};
+
+// The attention's plan, with splits of its own for more rows than a wave's: that one allows the next more than two workgroups a
+// compute unit, and a tree's rows are seldom a divisor of them (64 nodes x 7 heads x 4 over 196000 tokens, three tiles: 43 splits are
+// 516 workgroups, 329 us; 42 are 504, 217).  Costs as in c8_plan(); a round is two workgroups a compute unit, the last one's are alone if
+// they are no more than one.  A rest of up to 128 rows behind tiles of 192 has one or two tiles a wave, and fewer splits in the ratio of
+// what a block costs (those 448 rows: 49 splits of two tiles of 192, 30 of 64 rows, 205 us; 231 rows 160 -> 133).  As many splits as the workspace
+// holds, for which the size query walks all trees of up to n nodes.  (Trees of very different sizes leave tiles without rows, whose
+// workgroups end at once, and so more splits would do for them.)
+static TreePlan tree_plan(const C8Geom& g, int n, size_t ws_bytes) {
+  TreePlan t{c8_plan(g, n), 0, 0};
+  C8Plan& p = t.p;
+  if (p.few) return t;
+  const long long heads = (long long)g.H * g.B, rows = (long long)n * g.rep, cu = device_cu_count();
+  auto alone = [](int nt) { return 0.8f + 0.1f * nt; };
+  auto beside = [](int nt) { return nt == 1 ? 1.0f : nt == 2 ? 1.25f : 1.65f; };
+  const float blocks = (float)(g.nbc + (n + G - 1) / G), row_us = (float)heads * rows * (2 * 528 / 5e6f);
+  const long long held = (long long)(ws_bytes / (heads * rows * (D + 2) * sizeof(float)));
+  const int most = (int)std::min({256LL, (g.nbc + 7LL) / 8, std::max(1LL, held)});
+  const int full = (int)(rows / 192), rest = (int)(rows % 192), nt = rest <= 64 ? 1 : 2;
+  const bool mixes = p.nt == 3 && full > 0 && rest > 0 && rest <= 128;
   float least = 0.0f;
-  for (int k = 1, most = p.splits; k <= most; ++k) {
-    const long long all = wgs * k, rest = all % (2 * cu);
-    const float round = (float)(all / (2 * cu)) * beside + (rest == 0 ? 0.0f : rest <= cu ? alone : beside);
-    const float us = blocks / k * round + (k > 1 ? 4.0f + row_us * k : 0.0f);
-    if (k == 1 || us < least) { least = us; p.splits = k; }
+  int splits = 1;
+  // (splits beyond a round of workgroups are looked at where there is about one without)
+  const long long enough = p.tiles * heads > cu ? 8 * cu : 2 * cu, step = (mixes ? full : p.tiles) * heads;
+  for (int k = 1; k <= most && (k == 1 || step * (k - 1) < enough); ++k) {
+    const float merge = k > 1 ? 4.0f + row_us * k : 0.0f;
+    const long long all = p.tiles * heads * k, left = all % (2 * cu);
+    const float rounds = (float)(all / (2 * cu)) * beside(p.nt) + (left == 0 ? 0.0f : left <= cu ? alone(p.nt) : beside(p.nt));
+    const float us = blocks / k * rounds + merge;
+    if (k == 1 || us < least) { least = us; splits = k; t.few = 0; }
+    const int few = (int)ceilf(k * beside(nt) / beside(3));
+    const long long both = heads * (full * (long long)k + few);
+    const float mixed = blocks / k * (both <= cu ? alone(3) : beside(3)) + merge;
+    if (mixes && both <= 2 * cu && mixed < least) { least = mixed; splits = k; t.few = few; t.full = full; }
   }
-  return p;
+  p.splits = splits;
+  return t;
 }
 
 hipError_t launch_c8_tree(const C8Geom& g, int layer, int n, float scale, const vidkv_view* q, const vidkv_view* K, const vidkv_view* V,
                           const uint64_t* mask, const uint8_t* cache, const int32_t* length, const int32_t* count,
-                          const vidkv_view* out, void* ws, hipStream_t st) {
-  const C8Plan p = tree_plan(g, n);
+                          const vidkv_view* out, void* ws, size_t ws_bytes, hipStream_t st) {
+  const TreePlan plan = tree_plan(g, n, ws_bytes);
+  const C8Plan& p = plan.p;
   const C8Attn a = c8_args(g, p, layer, n, 0, scale, q, cache, length, count, out, ws);
   auto go = [&](auto t, auto code) {
     using T = decltype(t);
     constexpr int CODE = decltype(code)::value;
     const Tree<T> tree{make_view(K), make_view(V), reinterpret_cast<const uint32_t*>(mask), (n + 63) / 64 * 2};
     const dim3 blk(256), few(p.splits, g.H, g.B), many(p.tiles * p.splits * g.H * g.B);
-    if (p.few && p.waves == 12) hipLaunchKernelGGL((c8_tree_few_kernel<1, CODE, 12, T>), few, dim3(768), 0, st, a, tree);
+    if (plan.few) {
+      const dim3 mixed((unsigned)((long long)(plan.full * p.splits + plan.few) * g.H * g.B));
+      if (n * g.rep % 192 <= 64) hipLaunchKernelGGL((c8_tree_mixed_kernel<1, CODE, T>), mixed, blk, 0, st, a, tree, plan.full, plan.few);
+      else hipLaunchKernelGGL((c8_tree_mixed_kernel<2, CODE, T>), mixed, blk, 0, st, a, tree, plan.full, plan.few);
+    } else if (p.few && p.waves == 12) hipLaunchKernelGGL((c8_tree_few_kernel<1, CODE, 12, T>), few, dim3(768), 0, st, a, tree);
     else if (p.few && p.nt == 1) hipLaunchKernelGGL((c8_tree_few_kernel<1, CODE, 4, T>), few, blk, 0, st, a, tree);
     else if (p.few && p.nt == 2) hipLaunchKernelGGL((c8_tree_few_kernel<2, CODE, 4, T>), few, blk, 0, st, a, tree);
     else if (p.few) hipLaunchKernelGGL((c8_tree_few_kernel<3, CODE, 4, T>), few, blk, 0, st, a, tree);
