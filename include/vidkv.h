@@ -481,7 +481,8 @@ vidkv_status vidkv_tree_masks(int32_t batch, int32_t n_nodes, const int32_t *par
  *   q, out, K, V   : [B, Hq, n_nodes, 128] and [B, Hkv, n_nodes, 128], all fp16 or
  *                    all bf16
  *   mask_dev    in : [B, n_nodes, ceil(n_nodes / 64)] uint64, 8-byte aligned
- *   workspace_dev  : >= vidkv_cache8_workspace_bytes(p, n_nodes) bytes            */
+ *   workspace_dev  : >= vidkv_cache8_workspace_bytes(p, n_nodes) bytes; what more it
+ *                    holds can be used, which changes the order of sums           */
 vidkv_status vidkv_cache8_tree_attention(const vidkv_cache8 *p, int32_t layer, int32_t n_nodes,
                                          const vidkv_view *q, const vidkv_view *K,
                                          const vidkv_view *V, const uint64_t *mask_dev,
@@ -538,7 +539,8 @@ vidkv_status vidkv_tree_verify(int32_t batch, int32_t n_nodes, int32_t vocab,
 /* Appends nodes path[b][0 .. accepted[b] - 1] of all layers as tokens start[b],
  * start[b] + 1, ..., the same as vidkv_cache8_write of those rows in every layer
  * would.  K and V are those of layer 0; layer l's are l * k_stride_layer (V: v_stride_layer)
- * elements further on.
+ * elements further on.  Heads of all sequences and layers are fewer than 2^24 (else
+ * VIDKV_ESHAPE).
  *   K, V        in : [B, Hkv, n_nodes, 128], fp16 or bf16, both the same dtype, turned already
  *   path_dev    in : [B, n_nodes] int32, as vidkv_tree_verify leaves it: any nodes
  *                    in any order; the path ends before an entry outside 0..n_nodes-1

@@ -247,7 +247,7 @@ vidkv_status vidkv_cache8_append_path(const vidkv_cache8* p, int32_t n_nodes, co
                                       const int32_t* start, void* cache, size_t cache_bytes, void* stream) {
   C8Geom g;
   if (!p || !cache || !path || !accepted || !start) return VIDKV_EINVAL;
-  if (!make_c8(p, &g) || !good_nodes(n_nodes) || !c8_append_fits(g, n_nodes)) return VIDKV_ESHAPE;
+  if (!make_c8(p, &g) || !good_nodes(n_nodes) || !c8_append_fits(g)) return VIDKV_ESHAPE;
   if (!good_view(K, false) || !good_view(V, false) || K->dtype != V->dtype) return VIDKV_EINVAL;
   const int64_t most = (int64_t)1 << 48;
   for (int64_t s : {k_stride_layer, v_stride_layer})

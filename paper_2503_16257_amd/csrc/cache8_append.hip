@@ -34,7 +34,7 @@ __global__ __launch_bounds__(256) void c8_append_kernel(C8Write a, Path path) {
 }
 
 // Whether a grid holds an append to all layers: HIP counts a dimension's threads in 32 bits.
-bool c8_append_fits(const C8Geom& g, int) { return (unsigned __int128)g.H * g.B * g.L < (1 << 24); }
+bool c8_append_fits(const C8Geom& g) { return (unsigned __int128)g.H * g.B * g.L < (1 << 24); }
 
 hipError_t launch_c8_append(const C8Geom& g, int n, const vidkv_view* K, long long k_layer, const vidkv_view* V, long long v_layer,
                             const int32_t* path, const int32_t* count, const int32_t* start, uint8_t* cache, hipStream_t st) {

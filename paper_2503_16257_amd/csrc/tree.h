@@ -38,7 +38,7 @@ hipError_t launch_tree_verify(const TreeVerify& a, int dtype, int batch, void* w
 hipError_t launch_c8_tree(const C8Geom& g, int layer, int n, float scale, const vidkv_view* q, const vidkv_view* K, const vidkv_view* V,
                           const uint64_t* mask, const uint8_t* cache, const int32_t* length, const int32_t* count,
                           const vidkv_view* out, void* ws, size_t ws_bytes, hipStream_t st);
-bool c8_append_fits(const C8Geom& g, int n);
+bool c8_append_fits(const C8Geom& g);
 hipError_t launch_c8_append(const C8Geom& g, int n, const vidkv_view* K, long long k_layer, const vidkv_view* V, long long v_layer,
                             const int32_t* path, const int32_t* count, const int32_t* start, uint8_t* cache, hipStream_t st);
 

@@ -73,7 +73,7 @@ struct PF32 { typedef float E; static __device__ __forceinline__ float widen(E e
 struct PF16 { typedef _Float16 E; static __device__ __forceinline__ float widen(E e) { return (float)e; } };
 struct PBF16 { typedef __bf16 E; static __device__ __forceinline__ float widen(E e) { return (float)e; } };
 
-__device__ __forceinline__ double weight(float p, float q, double a) { return fmax((double)p - a * (double)q, 0.0); }
+__device__ __forceinline__ double weight(float p, float q, double a) { return fmax((double)p - a * (double)fmaxf(q, 0.0f), 0.0); }
 
 // A double from another lane of a row of sixteen, or of another row; zero where there is none.
 template <int CTRL, int ROWS = 0xf>
@@ -112,9 +112,10 @@ struct Walk {
   int node, last;              // the node reached, its last child that was tried (or itself)
   double a, b, used;           // the residual there; what the tried ones took of Q
   double further;              // a of the residual that a pass is to sum up
-  int pending;                 // ... which is asked for: else the walk is over
-  int summed;                  // b is that sum (where Q is): the residual's weights have been added up in a pass
+  int sums;                    // ASKED for with `further`; HERE: those of the residual's weights are made; or NONE_MADE.  If not asked
+                               // for, the walk is over
 };
+enum { NONE_MADE, HERE, ASKED };
 
 // Thread i loads node i; what does not depend on one another is asked for at once.  probs: the probabilities too, for a walk.
 struct NodeIn {
@@ -158,7 +159,6 @@ __device__ __forceinline__ void walk_on(Walk& w, const Nodes& s, bool drawn, boo
   int up[4], x[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) { up[j] = s.parent[lane + 64 * j]; x[j] = s.token[lane + 64 * j]; }
-  w.pending = 0;
   for (;;) {
     int child = -1;
 #pragma unroll
@@ -185,20 +185,26 @@ __device__ __forceinline__ void walk_on(Walk& w, const Nodes& s, bool drawn, boo
     if (u * (w.b * scale * q) < fmax(p - w.a * q, 0.0)) {
       w.node = w.last = child;
       w.a = 0.0; w.b = 1.0; w.used = 0.0;
-      w.summed = 0;
+      w.sums = NONE_MADE;
       continue;
     }
     w.used += q;
     w.further = w.a + w.b * scale;
-    w.pending = 1;
+    w.sums = ASKED;
     return;
   }
 }
 
+// The same for a wave's every lane, held as its scalars.
+__device__ __forceinline__ Walk uniform(const Walk& w) {
+  return Walk{__builtin_amdgcn_readfirstlane(w.node), __builtin_amdgcn_readfirstlane(w.last), lane_value(w.a, 0), lane_value(w.b, 0),
+              lane_value(w.used, 0), lane_value(w.further, 0), __builtin_amdgcn_readfirstlane(w.sums)};
+}
+
 // ... with the sum it asked for.  A residual of nothing is not taken: what was there before stays, and no further child is tried.
 __device__ __forceinline__ void take_sum(Walk& w, double z) {
-  w.summed = z > 0.0;
-  if (w.summed) { w.a = w.further; w.b = z; }
+  w.sums = z > 0.0 ? HERE : NONE_MADE;
+  if (z > 0.0) { w.a = w.further; w.b = z; }
   else w.last = VIDKV_TREE_NODES;
 }
 
@@ -335,7 +341,7 @@ __global__ __launch_bounds__(256) void tree_pass_kernel(TreeVerify a, TreeWork k
   if (count == 0) return;
   __shared__ Nodes s;
   __shared__ State next;
-  State from{Walk{0, 0, 0.0, 1.0, 0.0, 0.0, 0, 0}, 0, 0};
+  State from{Walk{0, 0, 0.0, 1.0, 0.0, 0.0, NONE_MADE}, 0, 0};
   if (round > 0) from = k.state[(size_t)(1 - now) * gridDim.y + b];
   if (from.done) {
     if (blockIdx.x == 0 && tid == 0) k.state[(size_t)now * gridDim.y + b] = from;
@@ -351,17 +357,17 @@ __global__ __launch_bounds__(256) void tree_pass_kernel(TreeVerify a, TreeWork k
   const bool drawn = a.draft.data != nullptr;
   if (wv == 0) {
     Walk w = from.w;
-    if (w.pending) take_sum(w, z);
+    if (w.sums == ASKED) take_sum(w, z);
     walk_on(w, s, drawn, a.distinct, lane);
-    State to{w, !w.pending, w.pending || !w.summed ? now : 1 - now};
+    State to{w, w.sums != ASKED, w.sums == HERE ? 1 - now : now};
     if (lane == 0) {
       next = to;
       if (blockIdx.x == 0) k.state[(size_t)now * gridDim.y + b] = to;
     }
   }
   __syncthreads();
-  const Walk w = next.w;
-  if (next.done && w.summed) return;       // (the sums of the launch before are the last ones)
+  const Walk w = uniform(next.w);
+  if (w.sums == HERE) return;       // (the sums of the launch before are the last ones)
   int tried[4] = {-1, -1, -1, -1};
   if (next.done) load_tried(tried, s, w.node, drawn, lane);
   sum_slabs(k.sums + ((size_t)now * gridDim.y + b) * k.slabs, row_of<T>(a, b, w.node, next.done ? w.a : w.further), tried,
@@ -386,7 +392,7 @@ __global__ __launch_bounds__(64 * W) void tree_finish_kernel(TreeVerify a, TreeW
     if (tid == 0) { a.accepted[b] = 0; a.next[b] = -1; }
     return;
   }
-  State from{Walk{0, 0, 0.0, 1.0, 0.0, 0.0, 0, 0}, 0, 0};
+  State from{Walk{0, 0, 0.0, 1.0, 0.0, 0.0, NONE_MADE}, 0, 0};
   if (rounds > 0) {
     const int last = (rounds - 1) & 1;
     from = k.state[(size_t)last * gridDim.x + b];
@@ -403,38 +409,43 @@ __global__ __launch_bounds__(64 * W) void tree_finish_kernel(TreeVerify a, TreeW
   __syncthreads();
   const bool drawn = a.draft.data != nullptr;
   Walk w = from.w;
-  bool have = from.done;                   // sums are those of the last node's weights
-  auto pass = [&](double with, const int (&tried)[4]) {
-    sum_slabs(sums, row_of<T>(a, b, w.node, with), tried, wv, W, slabs, lane);
-    __syncthreads();
-  };
   int tried[4] = {-1, -1, -1, -1};
-  if (!from.done) {
-    for (;;) {
-      if (w.pending) take_sum(w, total_of(sums, slabs, lane));
+  // whose sums are wanted: 0: what the walk asks for, 1: the last node's weights, 2: its row as it was, where nothing is left of it
+  int of = from.done ? 1 : 0;
+  bool here = from.done;                   // they are made already
+  double total = 0.0, with = w.a;
+  if (of) load_tried(tried, s, w.node, drawn, lane);
+  for (;;) {
+    if (of == 0) {
+      if (w.sums == ASKED) take_sum(w, total_of(sums, slabs, lane));
       if (wv == 0) {
         walk_on(w, s, drawn, a.distinct, lane);
         if (lane == 0) shared = w;
       }
       __syncthreads();
-      w = shared;
+      w = uniform(shared);
       __syncthreads();
-      if (!w.pending) break;
-      pass(w.further, tried);
+      with = w.further;
+      if (w.sums != ASKED) {
+        of = 1;
+        with = w.a;
+        here = w.sums == HERE;
+        load_tried(tried, s, w.node, drawn, lane);
+      }
     }
-    have = w.summed;
-  }
-  load_tried(tried, s, w.node, drawn, lane);
-  if (!have) pass(w.a, tried);
-  double total = total_of(sums, slabs, lane), with = w.a;
-  if (!(total > 0.0)) {                    // nothing left of it: the row as it was
+    if (!here) {
+      sum_slabs(sums, row_of<T>(a, b, w.node, with), tried, wv, W, slabs, lane);
+      __syncthreads();
+    }
+    here = false;
+    if (of == 0) continue;
+    total = total_of(sums, slabs, lane);
+    if (total > 0.0 || of == 2) break;
+    of = 2;
+    with = 0.0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) tried[j] = -1;
-    with = 0.0;
     __syncthreads();
-    sum_slabs(sums, row_of<T>(a, b, w.node, 0.0), tried, wv, W, slabs, lane);
-    __syncthreads();
-    total = total_of(sums, slabs, lane);
   }
   // the slab in which the sum passes u times the total, or the last one that has any
   const double goal = (double)s.u[0] * total;
@@ -492,10 +503,11 @@ __global__ __launch_bounds__(64 * W) void tree_finish_kernel(TreeVerify a, TreeW
     if (lane == 0) {
       a.next[b] = token;
       int depth = 0;
-      for (int i = w.node; i > 0; i = s.parent[i]) ++depth;
+      const int node = __builtin_amdgcn_readfirstlane(w.node);           // (a copy: the compiler chases w's address with the nodes')
+      for (int i = node; i > 0; i = s.parent[i]) ++depth;
       found = depth + 1;
       a.accepted[b] = depth + 1;
-      for (int i = w.node, d = depth; d >= 0; i = s.parent[i], --d) a.path[(size_t)b * a.n + d] = i;
+      for (int i = node, d = depth; d >= 0; i = s.parent[i], --d) a.path[(size_t)b * a.n + d] = i;
     }
   }
   __syncthreads();

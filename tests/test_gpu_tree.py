@@ -302,3 +302,45 @@ def test_append_ends_before_an_entry_that_is_no_node():
     for layer in range(2):
         vk.cache8_write(p, layer, want, K[layer], K[layer], i32([3, 3, 3]), i32([0, 40, 5]))
     assert torch.equal(got, want)
+
+
+def test_a_cache_beyond_32_bits():
+    """Two layers of 8 heads x 2^20 tokens, 8.6 GB: cleared, so tokens of zeros, but for the last ones of the second layer; nodes over all of
+    it, and a path appended at its end.  K: 1 for zeros; V: the last tokens' alone."""
+    L, H, cap, n = 4, 8, 1 << 20, 5
+    p = vk.make_cache8(L, 1, H, H, cap, 0)
+    buf = vk.alloc_bytes(vk.cache8_bytes(p), DEV)
+    buf.zero_()
+    assert buf.numel() > 1 << 33
+    g = torch.Generator(device=DEV)
+    g.manual_seed(3)
+    K, V, q = (torch.randn((1, H, t, 128), generator=g, device=DEV).half() for t in (64, 64, n))
+    q *= 4.0
+    vk.cache8_write(p, L - 1, buf, K, V, i32([cap - 64]))
+    Kt, Vt = (torch.randn((L, 1, H, n, 128), generator=g, device=DEV).half() for _ in range(2))
+    masks = torch.zeros((1, n, 1), dtype=torch.int64, device=DEV)
+    vk.tree_masks(i32([[-1, 0, 0, 1, 2]]), masks)
+    out = torch.empty_like(q)
+    ws = vk.alloc_bytes(vk.cache8_workspace_bytes(p, n), DEV)
+    vk.cache8_tree_attention(p, L - 1, buf, q, Kt[L - 1], Vt[L - 1], masks, out, i32([cap]), ws)
+    Kr, Vr = (torch.empty((1, H, 64, 128), device=DEV) for _ in range(2))
+    vk.cache8_read(p, L - 1, buf, i32([cap - 64]), Kr, Vr)
+    sees = O.masks(n, [-1, 0, 0, 1, 2], n)[0]
+    for h in range(H):
+        k = np.concatenate([f64(Kr)[0, h], f64(Kt)[L - 1, 0, h]])
+        v = np.concatenate([f64(Vr)[0, h], f64(Vt)[L - 1, 0, h]])
+        for i in range(n):
+            w = np.exp(SCALE * (k @ f64(q)[0, h, i])) * np.concatenate([np.ones(64), sees[i]])
+            ref, W = (w @ v) / (w.sum() + cap - 64), (w @ np.abs(v)) / (w.sum() + cap - 64)
+            # the module's bound: 2^20 weights of zeros' blocks are summed in float32, in 256 splits and waves
+            tol = W * (2.0 ** -11 + 2.0 ** -10 + 2.0 ** -24 * 40000) + 2.0 ** -11 * np.abs(ref) + 2.0 ** -25
+            assert (np.abs(f64(out)[0, h, i] - ref) <= tol).all(), (h, i)
+    before = [buf[:1 << 20].clone(), buf[-(1 << 20):].clone()]
+    vk.cache8_append_path(p, buf, Kt, Vt, i32([[0, 2, 4, -1, -1]]), i32([3]), i32([cap - 3]))
+    for layer in range(L):
+        back = torch.empty((1, H, 3, 128), device=DEV)
+        vk.cache8_read(p, layer, buf, i32([cap - 3]), back)
+        x = Kt[layer][:, :, [0, 2, 4]].float()
+        a = torch.maximum(x.abs().amax(dim=(2, 3), keepdim=True), K.float()[:, :, 32:].abs().amax(dim=(2, 3), keepdim=True) if layer == L - 1 else x.new_zeros(()))
+        assert ((back - x).abs() <= a * (0.5 / 127 * 1.0001)).all(), layer          # (half a step of the code)
+    assert torch.equal(before[0], buf[:1 << 20])

@@ -256,3 +256,41 @@ def test_shapes_that_do_not_fit_are_refused():
         vk.cache8_append_path(s.p, s.buf, s.K[:2], s.V, s.path, s.accepted, s.length)
     with pytest.raises(ValueError):
         vk.tree_masks(x["parents"], s.masks, s.length, s.pos[:, :2])
+
+
+@pytest.mark.parametrize("rule", ["certain", "distinct"])
+def test_the_same_with_and_without_the_native_call_layer(rule):
+    assert vk._native is not None
+    outs, native = [], vk._native
+    for layer in (native, None):
+        vk._native = layer
+        try:
+            s = Server(1, torch.bfloat16, rule, 49)
+            s.step()
+            vk.tree_masks(None, s.masks)
+            outs.append(s.results())
+        finally:
+            vk._native = native
+    assert same(*outs)
+
+
+def test_workspaces_of_several_sizes():
+    """What the size query says is enough, and more of it does no harm; one behind a call of more nodes neither."""
+    p = vk.make_cache8(1, 1, 2, 14, 4096, 0)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(50)
+    buf = vk.alloc_bytes(vk.cache8_bytes(p), DEV)
+    mk = lambda h, n: torch.randn((1, h, n, 128), generator=g, device=DEV).half()  # noqa: E731
+    vk.cache8_write(p, 0, buf, mk(2, 4000), mk(2, 4000), i32([0]))
+    for n in (1, 7, 8, 33, 64, 100):
+        q, K, V = mk(14, n), mk(2, n), mk(2, n)
+        masks = torch.zeros((1, n, (n + 63) // 64), dtype=torch.int64, device=DEV)
+        vk.tree_masks(None, masks)
+        outs = []
+        for size in (vk.cache8_workspace_bytes(p, n), vk.cache8_workspace_bytes(p, 256), 1 << 27):
+            ws = torch.full((size,), 255, dtype=torch.uint8, device=DEV)
+            out = torch.empty_like(q)
+            vk.cache8_tree_attention(p, 0, buf, q, K, V, masks, out, i32([4000]), ws)
+            outs.append(out.float())
+        # the same sums in other orders: 2^-11 of weights' roundings either way, of values of some units
+        assert max(float((o - outs[0]).abs().max()) for o in outs) <= 2.0 ** -9, n

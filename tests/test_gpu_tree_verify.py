@@ -169,6 +169,20 @@ def test_rows_without_weight():
 
 
 @pytest.mark.parametrize("rule", ["drawn", "distinct"])
+def test_entries_below_zero_and_nan_count_as_zero(rule):
+    t = Tree(20, 8, 1500, rule, F32, 16, agree=2.0)
+    want = Tree(20, 8, 1500, rule, F32, 16, agree=2.0)
+    for x, bad in ((t.target, -0.25), (t.draft, -0.125)):
+        x[:, :, 3::5] = bad
+    for x in (want.target, want.draft):
+        x[:, :, 3::5] = 0.0
+    want.check(t.run())
+    t.target[:, :, 4::50], want.target[:, :, 4::50] = float("nan"), 0.0
+    t.draft[:, :, 4::50], want.draft[:, :, 4::50] = float("nan"), 0.0
+    want.check(t.run())
+
+
+@pytest.mark.parametrize("rule", ["drawn", "distinct"])
 def test_equal_rows_leave_nothing(rule):
     """Target and draft are the same: whatever is turned down by a number that is none leaves the residual as it was."""
     t = Tree(6, 5, 700, rule, F32, 12, agree=0.0)
@@ -199,3 +213,24 @@ def test_large_vocabulary():
     for rule, V in (("certain", 1 << 22), ("drawn", 150001)):
         t = Tree(1, 3, V, rule, F16 if V > 200000 else F32, 14, branch=2, spread=2.0)
         t.check(t.run())
+
+
+def test_rows_beyond_32_bits():
+    """Probabilities of 2.4e9 entries, 4.8 GB: the rows that a path goes by lie at both ends."""
+    B, n, V = 40, 100, 600000
+    target = torch.zeros((B, n, V), dtype=F16, device=DEV)
+    tokens, parents = np.zeros((B, n), int), np.full((B, n), -1)
+    parents[:, 50:52], parents[:, 99] = 0, 51
+    tokens[:, 50], tokens[:, 51], tokens[:, 99] = 7, 599999, 300000
+    target[:, 0, 599999] = 1.0
+    target[:, 51, 300000] = 1.0
+    target[:, 99, 123456] = 0.5
+    target[:, 99, 599998] = 0.5
+    u = np.full((B, n), 0.25, np.float32)
+    u[1::2, 0] = 0.75
+    out = [torch.zeros((B, n), dtype=torch.int32, device=DEV)] + [torch.zeros((B,), dtype=torch.int32, device=DEV) for _ in range(2)]
+    vk.tree_verify(target, i32(tokens), torch.from_numpy(u).to(DEV), *out, vk.alloc_bytes(vk.tree_verify_workspace_bytes(B, n, V), DEV),
+                   parents=i32(parents))
+    path, accepted, token = (x.cpu().numpy() for x in out)
+    assert (accepted == 3).all() and (path[:, :4] == [0, 51, 99, -1]).all()
+    assert (token[::2] == 123456).all() and (token[1::2] == 599998).all()

@@ -106,7 +106,7 @@ def test_append_refuses():
         assert append(**{k: A + 2}) == vk.EINVAL, k
     assert append(c=A + 16) == vk.EINVAL and append(cb=vk.cache8_bytes(vk.make_cache8(2, 1, 4, 28, 64)) - 1) == vk.ENOSPACE
     assert append(n=0) == vk.ESHAPE and append(n=257) == vk.ESHAPE and append(p=vk.make_cache8(2, 1, 4, 28, 65)) == vk.ESHAPE
-    assert append(p=vk.make_cache8(1000, 1000, 8, 8, 512), n=40, cb=1 << 62) == vk.ESHAPE    # more workgroups than a grid holds
+    assert append(p=vk.make_cache8(3000, 1000, 8, 8, 512), cb=1 << 62) == vk.ESHAPE          # more workgroups than a grid holds
     assert vk.lib().vidkv_cache8_append_path(None, 5, view(), 8, view(), 8, A, A, A, A, BIG, None) == vk.EINVAL
 
 
@@ -136,3 +136,21 @@ def test_binding_refuses_host_tensors_and_shapes():
         vk.cache8_append_path(p, u8, x, x, i, one, one)
     with pytest.raises(TypeError):
         vk.cache8_append_path(p, u8, x[None], x[None], i, one, one)
+
+
+def test_odd_arguments_are_left_to_the_python_path():
+    """The native call layer takes plain arguments that pass, and no others."""
+    vk.lib()
+    m = vk._native
+    assert m.tree_masks(*[None] * 7) is None and m.tree_masks(1) is None
+    assert m.cache8_tree_attention(*[None] * 13) is None and m.tree_verify(*[None] * 13) is None and m.cache8_append_path(*[None] * 9) is None
+    with pytest.raises(TypeError):
+        m.bind_tree(1, 2)
+    x, i = torch.zeros((1, 2, 3, 128), dtype=torch.float16), torch.zeros((1, 3), dtype=torch.int32)
+    u, one, words = torch.zeros(4096, dtype=torch.uint8), torch.zeros(1, dtype=torch.int32), torch.zeros((1, 3, 1), dtype=torch.int64)
+    p, rot, f = vk.make_cache8(1, 1, 2, 2, 32), vk.make_rotary((64,)), torch.zeros((1, 3, 9))
+    assert m.tree_masks(i, words, None, None, None, vk._stream, None) is None                    # host tensors; foreign structures
+    assert m.tree_verify(f, i, torch.zeros((1, 3)), i, one, one, u, None, None, None, False, vk._stream, None) is None
+    for c in (p, bytes(C.sizeof(vk.VidkvCache8)), rot):
+        assert m.cache8_tree_attention(c, 0, u, x, x, x, words, x, one, u, None, vk._stream, None) is None
+        assert m.cache8_append_path(c, u, x[None], x[None], i, one, one, vk._stream, None) is None
