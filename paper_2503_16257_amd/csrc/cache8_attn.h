@@ -282,7 +282,7 @@ struct Tree {
   static constexpr bool ON = true;
   typedef T Type;
   // A kernel's second argument, read where it is asked for: held over the cached tokens it costs the scalar registers that their
-  // loop goes by (48 rows, 16 sequences of up to 6001 tokens: 29.4 us, 35 registers spilled).  Arguments lie behind each other.
+  // loop goes by (48 rows, 16 sequences of up to 6001 tokens: 29.4 us and 35 registers spilled, so 27.1).  Arguments lie behind each other.
   static __device__ __forceinline__ Tree argument() {
     typedef const __attribute__((address_space(4))) char* Args;
     Args p = (Args)__builtin_amdgcn_kernarg_segment_ptr();
@@ -502,8 +502,8 @@ __device__ __forceinline__ void few_rows(const C8Attn a) {
   Block f, g;
   __shared__ f4 so[W][16][D / 4 + 1];
   if (b0 < b1) load_block(f, a.kc, a.vc, a.km, a.vm, head + b0, lane);      // (on its way while the queries are laid out)
-  // A drafted block, the wave's last work, is asked for now too and waits in LDS (asked for at its turn: 48 rows of 16
-  // sequences 27.7 us).  NT tiles have at most two; a workgroup's second buffer is for the one that is not the last.
+  // A drafted block, the wave's last work, is asked for now too and waits in LDS (48 rows of 16 sequences of
+  // up to 6001 tokens 26 us; asked for at its turn 27.7).  NT tiles have at most two; a workgroup's second buffer is for the one that is not the last.
   constexpr int BUFS = TREE::ON ? NT == 1 ? 1 : 2 : 0;
   __shared__ u32x4 tree_keys[BUFS ? BUFS : 1][BUFS ? 512 : 1];
   auto tree_block = [&] {
@@ -662,7 +662,7 @@ __device__ __forceinline__ void many_rows(const C8Attn a, const ManySpan span, L
   }
   // drafted tokens: each wave lays a quarter of a block out in LDS, keys as the codes above, values of lane group w.  The first
   // block is asked for now and waits there; the others are asked for a block ahead, when the cached tokens are done (and the
-  // first too where three tiles a wave have no registers for it: 196000 tokens, 64 nodes 453 us with those spilled, 330 so).
+  // first too where three tiles a wave have no registers for it: 196000 tokens, 64 nodes 453 us with those spilled, 337 so).
   constexpr bool EARLY = TREE::ON && NT < 3;
   const int d0 = max(b0 - nb, 0), d1 = end - nb;
   auto& tree_ops = lds.tree_ops;
