@@ -510,21 +510,23 @@ typedef struct vidkv_rows {
  *                     uniform[i] Q(x) < R(x); else R becomes max(R - Q, 0)
  *   draft, distinct 1 children were drawn without putting back: likewise, and Q(x)
  *                     becomes 0 and Q is divided by what is left of it
- * and R is divided by its sum.  The walk goes on at a child that stands, with its rows, and ends where no
- * child does.  The next token is the first v with sum_{w <= v} R(w) > uniform[0] sum R (the
- * last with R(v) > 0 if there is none).  Without draft, and with distinct, a token that an earlier
- * sibling had is passed over, as is one outside 0..vocab-1.  Where nothing at
- * all would be left of R (with numbers in [0, 1): by rounding alone), with draft it stays what it was and no
- * further child is tried, without it is the target's row again.
- * Sums and decisions are in 64 bits.  Entries have to be finite; those not above 0 count as 0.
+ * and R is divided by its sum.  The walk goes on at a child that stands, with its rows,
+ * and ends where no child does.  The next token is the first v with
+ * sum_{w <= v} R(w) > uniform[0] sum R (the last with R(v) > 0 if there is none).
+ * Without draft, and with distinct, a token that an earlier sibling had is passed over;
+ * one outside 0..vocab-1 always is.  Where nothing at all would be left of R (with numbers
+ * in [0, 1): by rounding alone), with draft it stays what it was and no further child is
+ * tried, without it is the target's row again.
+ * Sums and decisions are in 64 bits.  Entries have to be finite; those not above 0 count
+ * as 0.
  *   target     in : probabilities behind each node.  draft: of target's dtype
  *   token_dev  in : [B, n_nodes] int32 (node 0's is not looked at)
  *   parent_dev in : [B, n_nodes] int32; outside 0..i-1: node i is no child.  NULL: a chain
  *   uniform_dev in: [B, n_nodes] float32, independent numbers in [0, 1)
  *   path_dev  out : [B, n_nodes] int32: node 0 and the nodes that stand, then -1
  *   accepted_dev out: [B] int32: the nodes of the path, 1 at least (0 where count[b] is 0)
- *   next_dev  out : [B] int32: the next token; -1 where count[b] is 0 or the last node's row has nothing
- *                   above 0
+ *   next_dev  out : [B] int32: the next token; -1 where count[b] is 0 or the last
+ *                   node's row has nothing above 0
  *   workspace_dev : >= vidkv_tree_verify_workspace_bytes(..) bytes, 256-byte aligned
  * The size query gives 0 for sizes outside 1..65535, 1..VIDKV_TREE_NODES and
  * 1..VIDKV_TREE_VOCAB (the call: VIDKV_ESHAPE). */
