@@ -509,7 +509,9 @@ typedef struct vidkv_rows {
  *   draft, distinct 0 each child was drawn from row u of draft, Q: x stands if
  *                     uniform[i] Q(x) < R(x); else R becomes max(R - Q, 0)
  *   draft, distinct 1 children were drawn without putting back: likewise, and Q(x)
- *                     becomes 0 and Q is divided by what is left of it
+ *                     becomes 0 and Q is divided by 1 less the row's probability of the
+ *                     tokens turned down; where that is not above 0 there is nothing that
+ *                     a further child could have come from, and none is tried
  * and R is divided by its sum.  The walk goes on at a child that stands, with its rows,
  * and ends where no child does.  The next token is the first v with
  * sum_{w <= v} R(w) > uniform[0] sum R (the last with R(v) > 0 if there is none).

@@ -78,22 +78,26 @@ def verify(target, draft, tokens, parents, count, uniform, distinct=False):
         return [], -1
     row = lambda x, u: np.where(x[u] > 0, x[u], 0.0)  # noqa: E731
     u, path, R, Q, had = 0, [0], row(target, 0), None if draft is None else row(draft, 0), set()
+    tried = 0.0                                                # the row's probability of the tokens that were turned down
     for i in range(1, count):
         x = int(tokens[i])
         if parent_of(parents, i) != u or not 0 <= x < V:
             continue
         if x in had and (draft is None or distinct):
             continue
+        if distinct and tried >= 1.0:
+            break                                              # nothing is left of Q that a further child could have come from
         had.add(x)
         stands = uniform[i] * (1.0 if Q is None else Q[x]) < R[x]
         if not stands and Q is not None and not (R > Q).any():
             break                                              # nothing would be left: R stays, no further child is tried
         _, after, q_after = turned_down(R, Q, x, distinct)
         if stands:
-            u, had = i, set()
+            u, had, tried = i, set(), 0.0
             path.append(i)
             R, Q = row(target, i), None if draft is None else row(draft, i)
         else:
+            tried += 0.0 if draft is None else row(draft, u)[x]
             R, Q = after, q_after
     if not R.sum() > 0:
         R = row(target, u)

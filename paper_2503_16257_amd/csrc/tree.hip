@@ -63,8 +63,9 @@ hipError_t launch_tree_masks(const TreeMasks& a, int batch, hipStream_t st) {
 // The residual distribution of a node after its first children were turned down is kept in closed form: with R_0 = P and
 // R' = max(R - s Q, 0) / sum, and max(max(x, 0) - y, 0) = max(x - y, 0) for y >= 0,
 //   R_k(v) = max(P(v) - a_k Q(v), 0) / b_k,   a_0 = 0, b_0 = 1,   a' = a + b s,   b' = sum_v max(P(v) - a' Q(v), 0),
-// s = 1, or, where siblings were drawn without putting back, 1 over what the tried ones left of Q.  (A token that was tried has
-// a' Q > P and stays at zero by itself.)  So a child turned down costs one pass over a row of P and Q, and nothing is written
+// s = 1, or, where siblings were drawn without putting back, 1 over what the tried ones left of Q (of nothing no further child is
+// tried: passing one over takes nothing from the target's probabilities, letting it stand without a chance to compare would).  (A
+// token that was tried has a' Q > P and stays at zero by itself.)  So a child turned down costs one pass over a row of P and Q, and nothing is written
 // back.  Without Q, R is P without the tried tokens, b what they left, and no pass is needed before the last.
 // All sums, a and b are in 64 bits: a decision next to a border is that of the definition.
 //
@@ -164,6 +165,7 @@ __device__ __forceinline__ void walk_on(Walk& w, const Nodes& s, bool drawn, boo
 #pragma unroll
   for (int j = 0; j < 4; ++j) { up[j] = s.parent[lane + 64 * j]; x[j] = s.token[lane + 64 * j]; }
   for (;;) {
+    if (distinct && !(w.used < 1.0)) return;         // nothing is left of Q that a further child could have come from
     int child = -1;
 #pragma unroll
     for (int j = 3; j >= 0; --j) {
@@ -185,7 +187,7 @@ __device__ __forceinline__ void walk_on(Walk& w, const Nodes& s, bool drawn, boo
       w.b = fmax(w.b - p, 0.0);
       continue;
     }
-    const double scale = !distinct ? 1.0 : w.used < 1.0 ? 1.0 / (1.0 - w.used) : 0.0;
+    const double scale = distinct ? 1.0 / (1.0 - w.used) : 1.0;
     if (u * (w.b * scale * q) < fmax(p - w.a * q, 0.0)) {
       w.node = w.last = child;
       w.a = 0.0; w.b = 1.0; w.used = 0.0;
