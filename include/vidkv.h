@@ -519,6 +519,13 @@ typedef struct vidkv_rows {
  * one outside 0..vocab-1 always is.  Where nothing at all would be left of R (with numbers
  * in [0, 1): by rounding alone), with draft it stays what it was and no further child is
  * tried, without it is the target's row again.
+ * All rows are taken to sum to one, as float32 rows of a softmax do to some 2^-20.  A draft
+ * row that sums to 1 + e puts |e| of a token's probability off, and with distinct
+ * |e| / (1 + e - t) behind tokens turned down that have t of the row: nothing is promised of
+ * distinct rows whose rounding is not small against 1 - t.  In 16 bits |e| is up to 2^-8
+ * (bf16) or 2^-11 and 2^-25 for each entry below 2^-14 (fp16), and t soon 0.99; where that
+ * matters, make such rows float32, divide them by their sums, and both draw from them and
+ * pass them.
  * Sums and decisions are in 64 bits.  Entries have to be finite; those not above 0 count
  * as 0.
  *   target     in : probabilities behind each node.  draft: of target's dtype

@@ -644,7 +644,8 @@ def tree_verify(target, tokens, uniform, path, accepted, next_token, workspace, 
     """vidkv_tree_verify: target [B,n,vocab] probabilities (float32, float16, bfloat16) behind each node, tokens [B,n] int32,
     uniform [B,n] float32 in [0, 1) -> path [B,n] (nodes that stand, then -1), accepted [B] (how many), next_token [B], all int32.
     draft [B,n,vocab]: what the children of each node were drawn from, with `distinct` without putting back; None: they are no
-    random ones.  parents None: chains."""
+    random ones.  parents None: chains.  Rows sum to one: with `distinct` a nearly certain draft's rows are better passed in float32 and
+    divided by their sums (vidkv.h says what others are off by)."""
     L = _lib or lib()
     if _native is not None:
         st = _native.tree_verify(target, tokens, uniform, path, accepted, next_token, workspace, draft, parents, count, distinct,

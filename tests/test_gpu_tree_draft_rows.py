@@ -78,3 +78,23 @@ def test_frequencies_behind_a_nearly_certain_draft(dtype):
         path, accepted, token = verify(*rows, tokens, np.tile([-1, 0, 0], (B, 1)), r.random((B, 3)).astype(np.float32))
         got += np.bincount(np.where(accepted > 1, tokens[np.arange(B), np.maximum(path[:, 1], 0)], token), minlength=V)
     assert (np.abs(got / (4 * B) - P) < 5 * np.sqrt(P * (1 - P) / (4 * B)) + abs(1 - 1 / Q.sum())).all(), got / (4 * B)
+
+
+@pytest.mark.parametrize("top", [0.985, 0.9985])
+def test_frequencies_of_rows_divided_by_their_sums(top):
+    """A draft whose rows are bfloat16, as float32 rows that sum to one: 200000 sequences, 5 standard deviations."""
+    r = np.random.default_rng(22)
+    B, V = 50000, 3
+    P = np.array([0.5, 0.1, 0.4])
+    Q = torch.tensor([top, 0.8 * (1 - top), 0.2 * (1 - top)], dtype=torch.float64).bfloat16().float()
+    Q = (Q / Q.sum()).double().numpy()
+    got = np.zeros(V)
+    for _ in range(4):
+        tokens = np.zeros((B, 3), int)
+        tokens[:, 1] = r.choice(V, B, p=Q / Q.sum())
+        left = np.where(np.arange(V) == tokens[:, 1:2], 0.0, Q)
+        tokens[:, 2] = ((left.cumsum(1) / left.sum(1, keepdims=True)) <= r.random((B, 1))).sum(1).clip(max=V - 1)
+        rows = [torch.from_numpy(np.broadcast_to(x, (B, 3, V)).copy()).float() for x in (P, Q)]
+        path, accepted, token = verify(*rows, tokens, np.tile([-1, 0, 0], (B, 1)), r.random((B, 3)).astype(np.float32))
+        got += np.bincount(np.where(accepted > 1, tokens[np.arange(B), np.maximum(path[:, 1], 0)], token), minlength=V)
+    assert (np.abs(got / (4 * B) - P) < 5 * np.sqrt(P * (1 - P) / (4 * B)) + 1e-6).all(), got / (4 * B)

@@ -95,3 +95,31 @@ def test_the_walk_ends_there():
     assert O.verify(P, Q, [0, 0, 1, 2], [-1, 0, 0, 0], 4, [0.5, 0.5, 0.5, 0.0], True) == ([0], 2)
     # drawn independently, each comes from the whole row
     assert O.verify(P, Q, [0, 0, 1, 2], [-1, 0, 0, 0], 4, [0.5, 0.5, 0.5, 0.0], False) == ([0, 3], 2)
+
+
+def draft_rows(dtype):
+    """Rows as a softmax in the type leaves them, from flat ones to nearly certain ones (their first entry below 1)."""
+    r = np.random.default_rng(31)
+    for top in (0.3, 0.7, 0.93, 0.985, 0.994):
+        rest = r.dirichlet(np.full(3, 0.8)) * (1.0 - top)
+        yield r.dirichlet(np.full(4, 0.7)), stored([top, *rest], dtype)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_what_a_row_that_does_not_sum_to_one_is_off_by(dtype):
+    """Two children: the first |e| / S of a token's probability at most, S = 1 + e; the second, behind x, is compared with
+    Q / (1 - Q(x)) and was drawn from Q / (S - Q(x)), a row of the sum (S - Q(x)) / (1 - Q(x)): |e| / (S - Q(x))."""
+    for P, Q in draft_rows(dtype):
+        S = Q.sum()
+        e = abs(S - 1.0)
+        off = np.abs(total(P, Q, 2) - P).max()
+        assert off <= e / S + sum(q / S * e / (S - q) for q in Q) + 1 / 4096, (Q, off)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_rows_divided_by_their_sums_in_float32_keep_the_promise(dtype):
+    """The same rows, converted and divided: what is left is float32's rounding, 2^-24 of each entry against the 2^-8 that is left of
+    the most certain row."""
+    for P, Q in [*draft_rows(dtype), (np.array([0.5, 0.1, 0.4]), stored([0.9985, 0.00125, 0.00025], dtype))]:
+        Q = (torch.from_numpy(Q).float() / torch.from_numpy(Q).float().sum()).double().numpy()
+        assert np.abs(total(P, Q, 2) - P).max() <= 1 / 4096 + 2.0 ** -14
