@@ -592,9 +592,12 @@ def tree_masks(parents, masks, base=None, positions=None, count=None, stream=Non
     axes = 0
     if positions is not None:
         axes = positions.shape[0] if isinstance(positions, _Tensor) and positions.dim() == 3 else -1
-    _check(L.vidkv_tree_masks(B, n, _arg(parents, _i32, "parents", (B, n)), _arg(count, _i32, "count", (B,)),
-                              _arg(masks, _i64, "masks", (B, n, (n + 63) // 64)), axes, _arg(base, _i32, "base", (B,)),
-                              _arg(positions, _i32, "positions", (axes, B, n)), _stream(stream)), "vidkv_tree_masks")
+    a = [_arg(parents, _i32, "parents", (B, n)), _arg(count, _i32, "count", (B,)),
+         _arg(masks, _i64, "masks", (B, n, (n + 63) // 64)), axes, _arg(base, _i32, "base", (B,)),
+         _arg(positions, _i32, "positions", (axes, B, n))]
+    if B == 0:
+        return
+    _check(L.vidkv_tree_masks(B, n, *a, _stream(stream)), "vidkv_tree_masks")
 
 
 def cache8_tree_attention(p: VidkvCache8, layer: int, cache, q, K, V, masks, out, length, workspace, count=None,
