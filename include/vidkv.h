@@ -481,8 +481,8 @@ vidkv_status vidkv_tree_masks(int32_t batch, int32_t n_nodes, const int32_t *par
  *   q, out, K, V   : [B, Hq, n_nodes, 128] and [B, Hkv, n_nodes, 128], all fp16 or
  *                    all bf16
  *   mask_dev    in : [B, n_nodes, ceil(n_nodes / 64)] uint64, 8-byte aligned
- *   workspace_dev  : >= vidkv_cache8_workspace_bytes(p, n_nodes) bytes; what more it
- *                    holds can be used, which changes the order of sums           */
+ *   workspace_dev  : >= vidkv_cache8_workspace_bytes(p, n_nodes) bytes; the order of
+ *                    sums does not depend on what more it holds                   */
 vidkv_status vidkv_cache8_tree_attention(const vidkv_cache8 *p, int32_t layer, int32_t n_nodes,
                                          const vidkv_view *q, const vidkv_view *K,
                                          const vidkv_view *V, const uint64_t *mask_dev,

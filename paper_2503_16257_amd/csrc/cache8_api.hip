@@ -210,11 +210,10 @@ vidkv_status vidkv_cache8_tree_attention(const vidkv_cache8* p, int32_t layer, i
   for (const vidkv_view* v : {q, K, V, out})
     if (!good_view(v, false) || v->dtype != q->dtype) return VIDKV_EINVAL;
   if (!at(cache, 256) || !at(ws, 256) || !at(length, 4) || !at(count, 4) || !at(mask, 8)) return VIDKV_EINVAL;
-  if (cache_bytes < g.total || ws_bytes < c8_attn_ws_need(g, n_nodes)) return VIDKV_ENOSPACE;
+  if (cache_bytes < g.total) return VIDKV_ENOSPACE;
   if (!stream_on_current_device(static_cast<hipStream_t>(stream))) return VIDKV_EINVAL;
-  const hipError_t e = launch_c8_tree(g, layer, n_nodes, p->softmax_scale, q, K, V, mask, static_cast<const uint8_t*>(cache), length,
-                                      count, out, ws, ws_bytes, static_cast<hipStream_t>(stream));
-  return e == hipSuccess ? VIDKV_OK : VIDKV_EHIP;
+  return launch_c8_tree(g, layer, n_nodes, p->softmax_scale, q, K, V, mask, static_cast<const uint8_t*>(cache), length, count, out, ws,
+                        ws_bytes, static_cast<hipStream_t>(stream));
 }
 
 size_t vidkv_tree_verify_workspace_bytes(int32_t batch, int32_t n_nodes, int32_t vocab) {

@@ -945,6 +945,8 @@ __device__ __forceinline__ ManySpan even_span(const C8Attn& a, int at, int tiles
 }
 
 C8Plan c8_plan(const C8Geom& g, int n);
+size_t c8_parts(const C8Geom& g, long long rows, int splits);
+size_t c8_attn_ws_bytes(const C8Geom& g, int n);
 // Arguments of a call whose plan it is, and the merge of its splits behind it (cache8_attn.hip).
 C8Attn c8_args(const C8Geom& g, const C8Plan& p, int layer, int n, int causal, float scale, const vidkv_view* q, const uint8_t* cache,
                const int32_t* length, const int32_t* q_count, const vidkv_view* out, void* ws);

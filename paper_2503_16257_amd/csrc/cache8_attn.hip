@@ -126,7 +126,7 @@ C8Plan c8_plan(const C8Geom& g, int n) {
 }
 
 // Bytes of a call's partials.
-static size_t c8_parts(const C8Geom& g, long long rows, int splits) {
+size_t c8_parts(const C8Geom& g, long long rows, int splits) {
   return splits > 1 ? align256((size_t)g.B * g.H * rows * splits * (D + 2) * sizeof(float)) : 0;
 }
 size_t c8_attn_ws_need(const C8Geom& g, int n) { return c8_parts(g, (long long)n * g.rep, c8_plan(g, n).splits) + 256; }

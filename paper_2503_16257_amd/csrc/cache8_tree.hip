@@ -50,45 +50,52 @@ struct TreePlan {
 // compute unit, and a tree's rows are seldom a divisor of them (64 nodes x 7 heads x 4 over 196000 tokens, three tiles: 43 splits are
 // 516 workgroups, 329 us; 42 are 504, 217).  Costs as in c8_plan(); a round is two workgroups a compute unit, the last one's are alone if
 // they are no more than one.  A rest of up to 128 rows behind tiles of 192 has one or two tiles a wave, and fewer splits in the ratio of
-// what a block costs (those 448 rows: 49 splits of two tiles of 192, 30 of 64 rows, 205 us; 231 rows 160 -> 133).  As many splits as the workspace
-// holds, for which the size query walks all trees of up to n nodes.  (Trees of very different sizes leave tiles without rows, whose
-// workgroups end at once, and so more splits would do for them.)
-static TreePlan tree_plan(const C8Geom& g, int n, size_t ws_bytes) {
+// what a block costs (those 448 rows: 49 splits of two tiles of 192, 30 of 64 rows, 205 us; 231 rows 160 -> 133).  No more splits than the
+// size query has room for, which walks the attention's calls of up to n queries (1 to 6 us of the host's time: asked only
+// for more than the attention's own splits, that are always there); whatever more a workspace holds, a call's sums keep their
+// order.  (Trees of very different sizes leave tiles without rows, whose workgroups end at once, and so more splits would do for them.)
+static TreePlan tree_plan(const C8Geom& g, int n) {
   TreePlan t{c8_plan(g, n), 0, 0};
   C8Plan& p = t.p;
   if (p.few) return t;
+  const int own = p.splits;
   const long long heads = (long long)g.H * g.B, rows = (long long)n * g.rep, cu = device_cu_count();
   auto alone = [](int nt) { return 0.8f + 0.1f * nt; };
   auto beside = [](int nt) { return nt == 1 ? 1.0f : nt == 2 ? 1.25f : 1.65f; };
   const float blocks = (float)(g.nbc + (n + G - 1) / G), row_us = (float)heads * rows * (2 * 528 / 5e6f);
-  const long long held = (long long)(ws_bytes / (heads * rows * (D + 2) * sizeof(float)));
-  const int most = (int)std::min({256LL, (g.nbc + 7LL) / 8, std::max(1LL, held)});
   const int full = (int)(rows / 192), rest = (int)(rows % 192), nt = rest <= 64 ? 1 : 2;
   const bool mixes = p.nt == 3 && full > 0 && rest > 0 && rest <= 128;
-  float least = 0.0f;
-  int splits = 1;
   // (splits beyond a round of workgroups are looked at where there is about one without)
   const long long enough = p.tiles * heads > cu ? 8 * cu : 2 * cu, step = (mixes ? full : p.tiles) * heads;
-  for (int k = 1; k <= most && (k == 1 || step * (k - 1) < enough); ++k) {
-    const float merge = k > 1 ? 4.0f + row_us * k : 0.0f;
-    const long long all = p.tiles * heads * k, left = all % (2 * cu);
-    const float rounds = (float)(all / (2 * cu)) * beside(p.nt) + (left == 0 ? 0.0f : left <= cu ? alone(p.nt) : beside(p.nt));
-    const float us = blocks / k * rounds + merge;
-    if (k == 1 || us < least) { least = us; splits = k; t.few = 0; }
-    const int few = (int)ceilf(k * beside(nt) / beside(3));
-    const long long both = heads * (full * (long long)k + few);
-    const float mixed = blocks / k * (both <= cu ? alone(3) : beside(3)) + merge;
-    if (mixes && both <= 2 * cu && mixed < least) { least = mixed; splits = k; t.few = few; t.full = full; }
+  auto cheapest = [&](long long most) {
+    float least = 0.0f;
+    for (int k = 1; k <= most && (k == 1 || step * (k - 1) < enough); ++k) {
+      const float merge = k > 1 ? 4.0f + row_us * k : 0.0f;
+      const long long all = p.tiles * heads * k, left = all % (2 * cu);
+      const float rounds = (float)(all / (2 * cu)) * beside(p.nt) + (left == 0 ? 0.0f : left <= cu ? alone(p.nt) : beside(p.nt));
+      const float us = blocks / k * rounds + merge;
+      if (k == 1 || us < least) { least = us; p.splits = k; t.few = 0; }
+      const int few = (int)ceilf(k * beside(nt) / beside(3));
+      const long long both = heads * (full * (long long)k + few);
+      const float mixed = blocks / k * (both <= cu ? alone(3) : beside(3)) + merge;
+      if (mixes && both <= 2 * cu && mixed < least) { least = mixed; p.splits = k; t.few = few; t.full = full; }
+    }
+  };
+  const long long most = std::min(256LL, (g.nbc + 7LL) / 8);
+  cheapest(most);
+  if (p.splits > own) {
+    const long long room = (long long)((c8_attn_ws_bytes(g, n) - 256) / (heads * rows * (D + 2) * sizeof(float)));
+    if (p.splits > room) cheapest(std::min(most, std::max(1LL, room)));
   }
-  p.splits = splits;
   return t;
 }
 
-hipError_t launch_c8_tree(const C8Geom& g, int layer, int n, float scale, const vidkv_view* q, const vidkv_view* K, const vidkv_view* V,
-                          const uint64_t* mask, const uint8_t* cache, const int32_t* length, const int32_t* count,
-                          const vidkv_view* out, void* ws, size_t ws_bytes, hipStream_t st) {
-  const TreePlan plan = tree_plan(g, n, ws_bytes);
+vidkv_status launch_c8_tree(const C8Geom& g, int layer, int n, float scale, const vidkv_view* q, const vidkv_view* K, const vidkv_view* V,
+                            const uint64_t* mask, const uint8_t* cache, const int32_t* length, const int32_t* count,
+                            const vidkv_view* out, void* ws, size_t ws_bytes, hipStream_t st) {
+  const TreePlan plan = tree_plan(g, n);
   const C8Plan& p = plan.p;
+  if (ws_bytes < c8_parts(g, (long long)n * g.rep, p.splits) + 256) return VIDKV_ENOSPACE;
   const C8Attn a = c8_args(g, p, layer, n, 0, scale, q, cache, length, count, out, ws);
   auto go = [&](auto t, auto code) {
     using T = decltype(t);
@@ -114,7 +121,7 @@ hipError_t launch_c8_tree(const C8Geom& g, int layer, int n, float scale, const 
   if (q->dtype == VIDKV_F16) by_code(TF16{});
   else by_code(TBF16{});
   launch_c8_merge(a, st);
-  return hipGetLastError();
+  return hipGetLastError() == hipSuccess ? VIDKV_OK : VIDKV_EHIP;
 }
 
 }  // namespace vidkv
