@@ -602,11 +602,13 @@ struct ManySpan {
   int b, h, tile0;             // the workgroup's first row
   int sp, splits;              // of the splits of its rows (the partials have a.splits)
 };
-template <class TREE, bool EARLY>
+// EARLY: a tree's first block waits here.  NT: the most tiles a wave.
+template <class TREE, bool EARLY, int NT>
 struct ManyLds {
   Op ops[2][16][64];           // 0..7: K, tile of tokens tt, channels j at 4 tt + j; 8..15: V, tile of channels
-  Op tree_ops[EARLY ? 16 : 1][64];
-  uint32_t tree_sees[2][4][TREE::ON ? 3 : 1][16];
+  // (arrays of nothing where they are not used)
+  Op tree_ops[EARLY ? 16 : 0][64];
+  uint32_t tree_sees[TREE::ON ? 2 : 0][4][NT][16];
 };
 template <int NT, int CODE, class TREE, class LDS>
 __device__ __forceinline__ void many_rows(const C8Attn a, const ManySpan span, LDS& lds) {

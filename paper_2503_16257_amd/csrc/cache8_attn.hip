@@ -11,7 +11,7 @@ __global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : NT < 3 ? 2 : 1) void c8_few
 
 template <int NT, int CODE>
 __global__ __launch_bounds__(256, 2) void c8_many_kernel(C8Attn a, int tiles) {
-  __shared__ ManyLds<NoTree, false> lds;
+  __shared__ ManyLds<NoTree, false, NT> lds;
   many_rows<NT, CODE, NoTree>(a, even_span<NT>(a, blockIdx.x, tiles), lds);
 }
 

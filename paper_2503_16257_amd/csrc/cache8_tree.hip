@@ -21,7 +21,7 @@ __global__ __launch_bounds__(64 * W, W > 4 ? W / 4 : NT < 3 ? 2 : 1) void c8_tre
 
 template <int NT, int CODE, class T>
 __global__ __launch_bounds__(256, 2) void c8_tree_many_kernel(C8Attn a, Tree<T>, int tiles) {
-  __shared__ ManyLds<Tree<T>, (NT < 3)> lds;
+  __shared__ ManyLds<Tree<T>, (NT < 3), NT> lds;
   many_rows<NT, CODE, Tree<T>>(a, even_span<NT>(a, blockIdx.x, tiles), lds);
 }
 
@@ -29,7 +29,7 @@ __global__ __launch_bounds__(256, 2) void c8_tree_many_kernel(C8Attn a, Tree<T>,
 // less time, and so the rest has fewer splits (`few` of a.splits).  Workgroups of the rest come first.
 template <int REST, int CODE, class T>
 __global__ __launch_bounds__(256, 2) void c8_tree_mixed_kernel(C8Attn a, Tree<T>, int full, int few) {
-  __shared__ ManyLds<Tree<T>, true> lds;
+  __shared__ ManyLds<Tree<T>, true, 3> lds;
   int at = blockIdx.x;
   const int h = at % a.H; at /= a.H;
   const int b = at % a.B; at /= a.B;
