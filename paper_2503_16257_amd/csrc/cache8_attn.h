@@ -294,6 +294,16 @@ struct Tree {
   int words;
 };
 
+// ... and the first one for what is left to do behind the blocks.
+template <class TREE>
+__device__ __forceinline__ C8Attn arguments(const C8Attn& a) {
+  if constexpr (!TREE::ON) return a;
+  typedef const __attribute__((address_space(4))) char* Args;
+  Args p = (Args)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const C8Attn*)(const char*)p;
+}
+
 // Nodes t0 .. t0 + 31 that a lane's rows see, as bits, of `nq` that there are.
 template <int NT, class T>
 __device__ __forceinline__ void load_sees(uint32_t (&sees)[NT], const Tree<T>& tree, const C8Attn& a, int b, int row0, int rows, int nq,
@@ -897,32 +907,34 @@ __device__ __forceinline__ void many_rows(const C8Attn a, const ManySpan span, L
       if (i + 1 < d1) put_tree(ops[(i + 1) & 1], i + 1);
     }
   }
+  const C8Attn e = arguments<TREE>(a);
+  const int all_rows = e.n * e.rep;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     int row = row0 + 16 * t + x;
     if (TREE::ON) asm volatile("" : "+v"(row));          // (as in load_sees)
     const f2 ml = row_stats(r, t);
-    if (row >= rows) continue;
-    if (a.po) {
-      const size_t at = (((size_t)b * a.H + h) * rows + row) * a.splits + sp;
+    if (row >= all_rows) continue;
+    if (e.po) {
+      const size_t at = (((size_t)b * e.H + h) * all_rows + row) * e.splits + sp;
 #pragma unroll
-      for (int m = 0; m < 8; ++m) reinterpret_cast<f4*>(a.po)[at * (D / 4) + 4 * m + kb] = r.o[t][m];
-      if (kb == 0) { a.pml[2 * at] = ml[0]; a.pml[2 * at + 1] = ml[1]; }
+      for (int m = 0; m < 8; ++m) reinterpret_cast<f4*>(e.po)[at * (D / 4) + 4 * m + kb] = r.o[t][m];
+      if (kb == 0) { e.pml[2 * at] = ml[0]; e.pml[2 * at + 1] = ml[1]; }
     } else {
-      const float l = ml[1], f = l != 0.0f ? a.inv_level / l : 0.0f;
+      const float l = ml[1], f = l != 0.0f ? e.inv_level / l : 0.0f;
 #pragma unroll
-      for (int m = 0; m < 8; ++m) put_out(a, b, h, row, 16 * m + 4 * kb, l != 0.0f ? r.o[t][m] * f : f4{0.f, 0.f, 0.f, 0.f});
+      for (int m = 0; m < 8; ++m) put_out(e, b, h, row, 16 * m + 4 * kb, l != 0.0f ? r.o[t][m] * f : f4{0.f, 0.f, 0.f, 0.f});
     }
   }
   if constexpr (TREE::ON) {
     // fewer splits than the partials have: one of nothing for each behind them
-    if (a.po && sp + span.splits < a.splits) {
+    if (e.po && sp + span.splits < e.splits) {
       for (int i = tid; i < 64 * NT * (D / 4); i += 256) {
         const int row = tile0 + i / (D / 4);
-        if (row >= rows) break;
-        const size_t at = (((size_t)b * a.H + h) * rows + row) * a.splits + sp + span.splits;
-        reinterpret_cast<f4*>(a.po)[at * (D / 4) + i % (D / 4)] = f4{0.f, 0.f, 0.f, 0.f};
-        if (i % (D / 4) == 0) { a.pml[2 * at] = NONE; a.pml[2 * at + 1] = 0.0f; }
+        if (row >= all_rows) break;
+        const size_t at = (((size_t)b * e.H + h) * all_rows + row) * e.splits + sp + span.splits;
+        reinterpret_cast<f4*>(e.po)[at * (D / 4) + i % (D / 4)] = f4{0.f, 0.f, 0.f, 0.f};
+        if (i % (D / 4) == 0) { e.pml[2 * at] = NONE; e.pml[2 * at + 1] = 0.0f; }
       }
     }
   }
