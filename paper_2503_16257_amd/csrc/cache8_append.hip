@@ -7,10 +7,11 @@
 namespace vidkv {
 
 // A workgroup a head of a sequence of a layer walks the blocks that the path reaches, mostly one.  28 x 64 x 4 heads, 64 nodes of which
-// 1 to 8 stand: 32 us for 52 MB read and 37 written (a begun block's value record is read and written whole: its bytes are in
-// the attention's order), half of a wave's time waiting for them.  (A workgroup for each block that 64 nodes could reach, most
-// of them without work: 51; live keys' codes asked for at once and not when they are to be coded anew: 34; two to five layers
-// a workgroup, or two more workgroups a compute unit with some registers spilled: the same.)  grid (H x B x L), heads fastest.
+// 1 to 8 stand: 41 us for 53 MB read and 38 written, 18 at a copy's rate (a begun block's value record is read and written whole: its
+// bytes are in the attention's order), half of a wave's time waiting for them; 32 to 34 on a cache that the call before has just appended
+// to.  On such a cache: a workgroup for each block that 64 nodes could reach, most of them without work, 51; live keys' codes
+// asked for at once and not when they are to be coded anew, 34; two to five layers a workgroup, or two more workgroups a compute
+// unit with some registers spilled, as this one.  grid (H x B x L), heads fastest.
 template <class T, int CODE>
 __global__ __launch_bounds__(256) void c8_append_kernel(C8Write a, Path path) {
   ask_arguments(a);
