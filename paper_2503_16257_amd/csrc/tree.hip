@@ -65,8 +65,8 @@ hipError_t launch_tree_masks(const TreeMasks& a, int batch, hipStream_t st) {
 //   R_k(v) = max(P(v) - a_k Q(v), 0) / b_k,   a_0 = 0, b_0 = 1,   a' = a + b s,   b' = sum_v max(P(v) - a' Q(v), 0),
 // s = 1, or, where siblings were drawn without putting back, 1 over what the tried ones left of Q (of nothing no further child is
 // tried: passing one over takes nothing from the target's probabilities, letting it stand without a chance to compare would).  (A
-// token that was tried has a' Q > P and stays at zero by itself.)  So a child turned down costs one pass over a row of P and Q, and nothing is written
-// back.  Without Q, R is P without the tried tokens, b what they left, and no pass is needed before the last.
+// token that was tried has a' Q > P and stays at zero by itself.)  So a child turned down costs one pass over a row of P and Q, and
+// nothing is written back.  Without Q, R is P without the tried tokens, b what they left, and no pass is needed before the last.
 // All sums, a and b are in 64 bits: a decision next to a border is that of the definition.
 //
 // Bound by round trips: nodes -> probabilities -> row -> slab.  A chain of 6 over 32000 float32 9 us in one launch; 16 trees of 64
